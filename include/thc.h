@@ -510,6 +510,104 @@ int topkc_gather_sum(const void* const* grads, thc_dtype dt, uint32_t W, uint64_
 int topkc_scatter_mean(const uint16_t* values, const uint32_t* indices, uint32_t J, uint32_t C, uint32_t W,
                        uint64_t n, float* out, void* stream);
 
+/* ---- where a gradient comes from: matrix products in 8-bit floating point with a scale for
+ * each block of 128, and the embedding -----------------------------------------------------
+ * Not steps of the paper: the operators of a language model's training step whose results the
+ * calls above exchange.  They keep the conventions at the top, and in addition:
+ *   - a matrix is given by a pointer, its sizes and `ld`, the distance between two rows in elements
+ *     (ld >= columns, THC_ERR_SIZE otherwise; the elements between two rows are not touched);
+ *   - they keep nothing in the process beyond the call, allocate nothing, and may run beside any
+ *     other call, each with a workspace of its own; a workspace may be in any state;
+ *   - sums are formed in fp32 in an order that depends on the sizes and tokens alone: the same
+ *     inputs give the same bits, on every run, replay and stream;
+ *   - a NaN or an infinity is not an error: it reaches the results as a NaN, see below.
+ *
+ * An 8-bit matrix of rows x cols has two buffers:
+ *   codes   rows * thc_fp8_row_bytes(cols) bytes: every row's codes, zeros up to a multiple of 128;
+ *           THC_E4M3: 1 sign, 4 exponent (bias 7), 3 fraction bits, largest value 448, no infinity;
+ *           THC_E5M2: 1, 5 (bias 15) and 2 bits, largest value 57344
+ *   scales  thc_fp8_scale_bytes(rows, cols) bytes: block j = c / 128 of row r has the scale
+ *           2^(e - 127), e the byte (j % 4) of the 32-bit word (j / 4) * rows + r; 255 stands for NaN
+ *           (bytes of blocks behind the last one are written as 0 and not read)
+ * and stands for the values code * 2^(e - 127).  The scale is a power of two, so that scaling never
+ * rounds: e is the smallest byte for which the block's largest magnitude amax does not exceed the
+ * format's largest value times 2^(e - 127) (0 for an amax of up to 1.75 * 2^-119 with e4m3,
+ * 1.75 * 2^-112 with e5m2), and a code is the value times 2^(127 - e), rounded to nearest, ties to
+ * even.  A block with a NaN or an infinity gets e = 255 and the NaN code 0x7F throughout.  Both buffers 16-byte aligned. */
+enum { THC_E4M3 = 0, THC_E5M2 = 1 };
+enum { THC_I32 = 0, THC_I64 = 1 };   /* type of token indices, signed */
+
+/* Bytes of one row of codes: cols rounded up to a multiple of 128.  0 if cols > 2^22. */
+uint64_t thc_fp8_row_bytes(uint64_t cols);
+
+/* 4 * rows * ceil(cols / 512).  0 if a size is out of range (rows > 2^31 - 1, cols > 2^22). */
+uint64_t thc_fp8_scale_bytes(uint64_t rows, uint64_t cols);
+
+/* Quantize a matrix, its transpose, or both in one pass over it.
+ *   x         rows x cols of type dt, ld
+ *   format    THC_E4M3 / THC_E5M2 (THC_ERR_DTYPE otherwise)
+ *   tile      0: a block is 128 values along the row (of q; along the column of x for q_t)
+ *             else: one scale for each 128 x 128 tile, so that q and q_t hold the same values
+ *   q, scales      8-bit matrix of rows x cols, or both NULL
+ *   q_t, scales_t  8-bit matrix of cols x rows (the transpose), or both NULL; not all four NULL
+ * rows, cols <= 2^31 - 1 and <= 2^22 where they are contracted (cols with q, rows with q_t):
+ * THC_ERR_SIZE.  rows == 0 or cols == 0: a no-op. */
+int thc_fp8_quantize(const void* x, thc_dtype dt, uint64_t rows, uint64_t cols, uint64_t ld, int format, int tile,
+                     uint8_t* q, uint8_t* scales, uint8_t* q_t, uint8_t* scales_t, void* stream);
+
+/* out[r][c] = code * 2^(e - 127), rounded once to out_dt where bf16 cannot hold it. */
+int thc_fp8_dequantize(const uint8_t* q, const uint8_t* scales, int format, uint64_t rows, uint64_t cols,
+                       thc_dtype out_dt, void* out, uint64_t ld, void* stream);
+
+/* C = A B^T, or C += A B^T:
+ *     c[m][n] = (accumulate ? c[m][n] : 0) + sum over k < K of A[m][k] * B[n][k]
+ * over the values that the 8-bit matrices stand for, summed in fp32 and rounded once to out_dt (accumulate:
+ * with the old value added in fp32 before).
+ *   out_dt THC_F32: products are exact; a value beyond the normal range of fp32 counts as zero or infinite.
+ *   out_dt THC_BF16: of the products of 8 neighbouring k what lies more than 2^13 below the largest of them may be
+ *   cut off (the 8-bit matrix instruction; on normally distributed values 1.5e-5 in the 2-norm, of
+ *   the 1.7e-3 that the rounding to bf16 costs).
+ *   a, a_scales   8-bit matrix of M x K;   b, b_scales   8-bit matrix of N x K
+ *   c             M x N of out_dt, ldc
+ *   workspace     thc_fp8_matmul_workspace_bytes(M, N, K) bytes, 16-byte aligned; may be NULL if that is 0
+ * A linear layer with weights W (N x K) has  y = x W^T,  dx = dy (W^T)^T  (contracted over N) and
+ * dW = (dy^T) (x^T)^T  (contracted over the tokens): thc_fp8_quantize writes every operand in the
+ * form that is wanted.  M, N <= 2^31 - 1, K <= 2^22 (THC_ERR_SIZE).  K == 0: an empty sum. */
+uint64_t thc_fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
+int thc_fp8_matmul(const uint8_t* a, const uint8_t* a_scales, int a_format, const uint8_t* b, const uint8_t* b_scales,
+                   int b_format, uint64_t M, uint64_t N, uint64_t K, int accumulate, thc_dtype out_dt, void* c,
+                   uint64_t ldc, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* out = Q(x) B^T: thc_fp8_quantize (tile = 0) of the M x K matrix x into the workspace, then
+ * thc_fp8_matmul; the same results, bit for bit, with fewer launches for few rows.
+ *   workspace   thc_fp8_linear_workspace_bytes(M, N, K) bytes, 16-byte aligned; may be NULL if that is 0 */
+uint64_t thc_fp8_linear_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
+int thc_fp8_linear(const void* x, thc_dtype dt, uint64_t M, uint64_t K, uint64_t ldx, int x_format, const uint8_t* b,
+                   const uint8_t* b_scales, int b_format, uint64_t N, thc_dtype out_dt, void* out, uint64_t ldo,
+                   void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Embedding lookup: out[i] = scale * table[tokens[i]], the product in fp32, rounded once to out_dt.
+ * A token outside [0, vocab) (a padding mark, -1 for instance) gives a row of zeros.
+ *   table    vocab x dim of type dt, ld;   tokens   count indices of type index (THC_I32 / THC_I64,
+ *            THC_ERR_DTYPE otherwise);   out   count x dim of out_dt, ldo
+ * count, vocab, dim <= 2^31 - 1 (THC_ERR_SIZE). */
+int thc_embed_forward(const void* table, thc_dtype dt, uint64_t vocab, uint64_t dim, uint64_t ld, const void* tokens,
+                      int index, uint64_t count, float scale, thc_dtype out_dt, void* out, uint64_t ldo, void* stream);
+
+/* Its gradient: for every v < vocab
+ *     grad_table[v] = (accumulate ? grad_table[v] : 0) + scale * sum over i with tokens[i] = v of grad_out[i]
+ * Tokens are sorted on the device; rows of equal tokens are summed in fp32, multiplied by scale and rounded
+ * once to out_dt.  Without accumulate every row of grad_table is written (zeros for a token that does not
+ * occur), with it only rows of tokens that occur are touched.  Tokens outside [0, vocab) add nothing.
+ *   grad_out     count x dim of type dt, ld
+ *   grad_table   vocab x dim of out_dt, ldt
+ *   workspace    thc_embed_backward_workspace_bytes(count, vocab, dim) bytes, 16-byte aligned
+ * count, dim <= 2^31 - 1, vocab <= 2^31 - 1, count * dim < 2^44 (THC_ERR_SIZE). */
+uint64_t thc_embed_backward_workspace_bytes(uint64_t count, uint64_t vocab, uint64_t dim);
+int thc_embed_backward(const void* grad_out, thc_dtype dt, uint64_t ld, const void* tokens, int index, uint64_t count,
+                       uint64_t vocab, uint64_t dim, float scale, int accumulate, thc_dtype out_dt, void* grad_table,
+                       uint64_t ldt, void* workspace, uint64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

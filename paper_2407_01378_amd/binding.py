@@ -17,6 +17,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libthc.so")
 
 THC_F32, THC_BF16 = 0, 1
+THC_E4M3, THC_E5M2 = 0, 1
+THC_I32, THC_I64 = 0, 1
 THC_OK = 0
 
 _lib = None
@@ -167,6 +169,33 @@ _SIGNATURES = {
                                                 ctypes.c_uint64, ctypes.c_uint32, ctypes.c_uint64,
                                                 ctypes.c_uint32, ctypes.c_void_p, ctypes.c_void_p,
                                                 ctypes.c_void_p, ctypes.c_void_p]),
+    "thc_fp8_row_bytes": (ctypes.c_uint64, [ctypes.c_uint64]),
+    "thc_fp8_scale_bytes": (ctypes.c_uint64, [ctypes.c_uint64, ctypes.c_uint64]),
+    "thc_fp8_quantize": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64, ctypes.c_uint64,
+                                        ctypes.c_uint64, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    "thc_fp8_dequantize": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64,
+                                          ctypes.c_uint64, ctypes.c_int, ctypes.c_void_p, ctypes.c_uint64,
+                                          ctypes.c_void_p]),
+    "thc_fp8_matmul_workspace_bytes": (ctypes.c_uint64, [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint64]),
+    "thc_fp8_matmul": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p,
+                                      ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64, ctypes.c_uint64,
+                                      ctypes.c_uint64, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                      ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
+    "thc_fp8_linear_workspace_bytes": (ctypes.c_uint64, [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint64]),
+    "thc_fp8_linear": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64, ctypes.c_uint64,
+                                      ctypes.c_uint64, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                      ctypes.c_int, ctypes.c_uint64, ctypes.c_int, ctypes.c_void_p,
+                                      ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
+    "thc_embed_forward": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64, ctypes.c_uint64,
+                                         ctypes.c_uint64, ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64,
+                                         ctypes.c_float, ctypes.c_int, ctypes.c_void_p, ctypes.c_uint64,
+                                         ctypes.c_void_p]),
+    "thc_embed_backward_workspace_bytes": (ctypes.c_uint64, [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint64]),
+    "thc_embed_backward": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64, ctypes.c_void_p,
+                                          ctypes.c_int, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint64,
+                                          ctypes.c_float, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                          ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p]),
 }
 
 
@@ -768,3 +797,174 @@ def topkc_scatter_mean(values, indices, J, C, W, out, stream=None):
     return out
 
 
+
+
+# ------------------------------------- 8-bit matrices with a scale per block of 128, embedding
+# Tensors of these entry points are checked: types, shapes, sizes of the buffers, and that all of them are on one
+# GPU; the call is issued for that GPU (on its current stream where none is given), whichever is the current one.
+def _matrix(t, name, shape=None):
+    """A two-dimensional tensor whose rows are contiguous; returns the distance between rows."""
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected a matrix" + (f" of {shape[0]} x {shape[1]}" if shape is not None else "")
+                         + f", got {tuple(t.shape)}")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else cols
+    if (cols > 1 and rows and t.stride(1) != 1) or (cols and ld < cols):
+        raise ValueError(f"{name}: the rows of the matrix must be contiguous and must not overlap")
+    return max(ld, cols)
+
+
+def _bytes(t, name, count):
+    if t.dtype != torch.uint8 or not t.is_contiguous():
+        raise TypeError(f"{name}: expected contiguous uint8")
+    if t.numel() < count:
+        raise ValueError(f"{name}: {count} bytes are needed, got {t.numel()}")
+
+
+def _fp8_matrix(codes, scales, name, rows, cols):
+    _bytes(codes, name, rows * thc_fp8_row_bytes(cols))
+    _bytes(scales, name + " scales", thc_fp8_scale_bytes(rows, cols))
+
+
+def _scratch(workspace):
+    """Pointer and bytes of a workspace, which may be None."""
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def _index_code(tokens):
+    if tokens.dim() != 1 or not tokens.is_contiguous():
+        raise ValueError("tokens: expected a contiguous 1-D tensor")
+    if tokens.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"tokens: {tokens.dtype} is not int32 or int64")
+    return THC_I64 if tokens.dtype == torch.int64 else THC_I32
+
+
+def _on_device(name, stream, tensors, call):
+    """call(stream) with the tensors' GPU as the current one."""
+    tensors = [t for t in tensors if t is not None]
+    device = tensors[0].device
+    if device.type != "cuda" or any(t.device != device for t in tensors):
+        raise ValueError(f"{name}: all tensors must be on one GPU")
+    with torch.cuda.device(device):
+        _check(call(_stream(stream)), name)
+
+
+def thc_fp8_row_bytes(cols):
+    return lib().thc_fp8_row_bytes(cols)
+
+
+def thc_fp8_scale_bytes(rows, cols):
+    return lib().thc_fp8_scale_bytes(rows, cols)
+
+
+def thc_fp8_quantize(x, format, q=None, scales=None, q_t=None, scales_t=None, tile=False, stream=None):
+    """x (rows x cols, fp32 or bf16) to 8 bits: (q, scales) along its rows, (q_t, scales_t) its transpose."""
+    rc = (_native or _load_native()).thc_fp8_quantize(x, format, q, scales, q_t, scales_t, tile, stream)
+    if rc is None:
+        dt, ld = _dtype_code(x), _matrix(x, "x")
+        rows, cols = x.shape
+        if (q is None) != (scales is None) or (q_t is None) != (scales_t is None):
+            raise ValueError("codes and scales are given together")
+        if q is not None:
+            _fp8_matrix(q, scales, "q", rows, cols)
+        if q_t is not None:
+            _fp8_matrix(q_t, scales_t, "q_t", cols, rows)
+        _on_device("thc_fp8_quantize", stream, [x, q, scales, q_t, scales_t], lambda s: lib().thc_fp8_quantize(
+            _ptr(x), dt, rows, cols, ld, format, int(bool(tile)), _ptr(q), _ptr(scales), _ptr(q_t), _ptr(scales_t), s))
+    else:
+        _check(rc, "thc_fp8_quantize")
+    return q, scales, q_t, scales_t
+
+
+def thc_fp8_dequantize(q, scales, format, out, stream=None):
+    """The values of the 8-bit matrix of out's shape, in out (fp32 or bf16)."""
+    rc = (_native or _load_native()).thc_fp8_dequantize(q, scales, format, out, stream)
+    if rc is None:
+        dt, ld = _dtype_code(out), _matrix(out, "out")
+        _fp8_matrix(q, scales, "q", *out.shape)
+        _on_device("thc_fp8_dequantize", stream, [q, scales, out], lambda s: lib().thc_fp8_dequantize(
+            _ptr(q), _ptr(scales), format, out.shape[0], out.shape[1], dt, _ptr(out), ld, s))
+    else:
+        _check(rc, "thc_fp8_dequantize")
+    return out
+
+
+def thc_fp8_matmul_workspace_bytes(M, N, K):
+    return lib().thc_fp8_matmul_workspace_bytes(M, N, K)
+
+
+def thc_fp8_matmul(a, a_scales, a_format, b, b_scales, b_format, K, c, workspace=None, accumulate=False, stream=None):
+    """c (M x N, fp32 or bf16) = or += A B^T of the 8-bit matrices A (M x K) and B (N x K)."""
+    rc = (_native or _load_native()).thc_fp8_matmul(a, a_scales, a_format, b, b_scales, b_format, K, c, workspace,
+                                                    accumulate, stream)
+    if rc is None:
+        dt, ldc = _dtype_code(c), _matrix(c, "c")
+        M, N = c.shape
+        _fp8_matrix(a, a_scales, "a", M, K)
+        _fp8_matrix(b, b_scales, "b", N, K)
+        ws, bytes_ = _scratch(workspace)
+        _on_device("thc_fp8_matmul", stream, [a, a_scales, b, b_scales, c, workspace], lambda s: lib().thc_fp8_matmul(
+            _ptr(a), _ptr(a_scales), a_format, _ptr(b), _ptr(b_scales), b_format, M, N, K, int(bool(accumulate)), dt,
+            _ptr(c), ldc, ws, bytes_, s))
+    else:
+        _check(rc, "thc_fp8_matmul")
+    return c
+
+
+def thc_fp8_linear_workspace_bytes(M, N, K):
+    return lib().thc_fp8_linear_workspace_bytes(M, N, K)
+
+
+def thc_fp8_linear(x, x_format, b, b_scales, b_format, out, workspace=None, stream=None):
+    """out (M x N) = Q(x) B^T of x (M x K, fp32 or bf16) and the 8-bit matrix B (N x K)."""
+    rc = (_native or _load_native()).thc_fp8_linear(x, x_format, b, b_scales, b_format, out, workspace, stream)
+    if rc is None:
+        dt, ldx = _dtype_code(x), _matrix(x, "x")
+        out_dt, ldo = _dtype_code(out), _matrix(out, "out", (x.shape[0], out.shape[-1] if out.dim() else 0))
+        M, K, N = x.shape[0], x.shape[1], out.shape[1]
+        _fp8_matrix(b, b_scales, "b", N, K)
+        ws, bytes_ = _scratch(workspace)
+        _on_device("thc_fp8_linear", stream, [x, b, b_scales, out, workspace], lambda s: lib().thc_fp8_linear(
+            _ptr(x), dt, M, K, ldx, x_format, _ptr(b), _ptr(b_scales), b_format, N, out_dt, _ptr(out), ldo, ws, bytes_, s))
+    else:
+        _check(rc, "thc_fp8_linear")
+    return out
+
+
+def thc_embed_forward(table, tokens, scale, out, stream=None):
+    """out[i] = scale * table[tokens[i]]; zeros for a token outside the table."""
+    rc = (_native or _load_native()).thc_embed_forward(table, tokens, scale, out, stream)
+    if rc is None:
+        dt, ld, index = _dtype_code(table), _matrix(table, "table"), _index_code(tokens)
+        out_dt, ldo = _dtype_code(out), _matrix(out, "out", (tokens.numel(), table.shape[1]))
+        _on_device("thc_embed_forward", stream, [table, tokens, out], lambda s: lib().thc_embed_forward(
+            _ptr(table), dt, table.shape[0], table.shape[1], ld, _ptr(tokens), index, tokens.numel(), float(scale), out_dt,
+            _ptr(out), ldo, s))
+    else:
+        _check(rc, "thc_embed_forward")
+    return out
+
+
+def thc_embed_backward_workspace_bytes(count, vocab, dim):
+    return lib().thc_embed_backward_workspace_bytes(count, vocab, dim)
+
+
+def thc_embed_backward(grad_out, tokens, scale, grad_table, workspace, accumulate=False, stream=None):
+    """grad_table[v] = or += scale * the sum of the rows of grad_out whose token is v."""
+    rc = (_native or _load_native()).thc_embed_backward(grad_out, tokens, scale, grad_table, workspace, accumulate, stream)
+    if rc is None:
+        out_dt, ldt, index = _dtype_code(grad_table), _matrix(grad_table, "grad_table"), _index_code(tokens)
+        vocab, dim = grad_table.shape
+        dt, ld = _dtype_code(grad_out), _matrix(grad_out, "grad_out", (tokens.numel(), dim))
+        ws, bytes_ = _scratch(workspace)
+        _on_device("thc_embed_backward", stream, [grad_out, tokens, grad_table, workspace],
+                   lambda s: lib().thc_embed_backward(
+                       _ptr(grad_out), dt, ld, _ptr(tokens), index, tokens.numel(), vocab, dim, float(scale),
+                       int(bool(accumulate)), out_dt, _ptr(grad_table), ldt, ws, bytes_, s))
+    else:
+        _check(rc, "thc_embed_backward")
+    return grad_table

@@ -23,6 +23,7 @@ enum Entry {
     kSatEncodeAll, kSatEncodeAllCleared, kEncodeAllStatic, kWorkspaceClear, kAggregateDecode, kSatAggregateDecode,
     kEncodeAllMinmax, kAggregateDecodeMinmax, kEncodeAllBatch, kAggregateDecodeBatch, kForwardFullDeferred,
     kFullEncodeDeferred, kFullDecodeInverse, kTopkcNorms, kTopkcSumNorms, kTopkcSelect, kTopkcGather, kTopkcScatter,
+    kFp8Quantize, kFp8Dequantize, kFp8Matmul, kFp8Linear, kEmbedForward, kEmbedBackward,
     kEntries
 };
 const char* const kNames[kEntries] = {
@@ -31,7 +32,9 @@ const char* const kNames[kEntries] = {
     "thc_encode_all_static", "thc_workspace_clear", "thc_aggregate_decode", "thc_sat_aggregate_decode",
     "thc_encode_all_minmax", "thc_aggregate_decode_minmax", "thc_encode_all_batch", "thc_aggregate_decode_batch",
     "rht_forward_full_deferred", "thc_full_encode_deferred", "thc_full_decode_inverse", "topkc_chunk_norms",
-    "topkc_sum_norms", "topkc_select", "topkc_gather_sum", "topkc_scatter_mean"};
+    "topkc_sum_norms", "topkc_select", "topkc_gather_sum", "topkc_scatter_mean",
+    "thc_fp8_quantize", "thc_fp8_dequantize", "thc_fp8_matmul", "thc_fp8_linear", "thc_embed_forward",
+    "thc_embed_backward"};
 void* g_entry[kEntries];   // addresses in the loaded library, set once by bind()
 
 template <typename F>
@@ -561,6 +564,193 @@ THC_FN(topkc_scatter_mean_) {   // values, indices, J, C, W, out, stream
     return finish(c, [&] { return entry<decltype(topkc_scatter_mean)>(kTopkcScatter)(values, idx, J, C, W, count, out, s); });
 }
 
+// ---- 8-bit matrices and the embedding: tensors that the binding's checks would let pass, all of them on the
+// current GPU.
+constexpr uint64_t kMost = 0x7FFFFFFFull;   // a size beyond it is the library's to refuse
+struct Operands {
+    Args& c;
+    int device = -1;
+
+    explicit Operands(Args& args) : c(args) {
+        if (c.ok) device = (int)c10::hip::current_device();
+    }
+    const at::Tensor* any(int i) {
+        const at::Tensor* t = c.tensor(i);
+        if (t && (!t->is_cuda() || t->get_device() != device)) c.ok = false;
+        return t;
+    }
+    struct Matrix {
+        void* p = nullptr;
+        uint64_t rows = 0, cols = 0, ld = 0;
+        int dt = THC_F32;
+    };
+    Matrix matrix(int i) {
+        Matrix m;
+        const at::Tensor* t = any(i);
+        if (!c.ok || t->dim() != 2) {
+            c.ok = false;
+            return m;
+        }
+        const int64_t rows = t->size(0), cols = t->size(1);
+        if (rows < 1 || cols < 1 || rows > (int64_t)kMost || cols > (int64_t)kMost || (cols > 1 && t->stride(1) != 1) ||
+            (rows > 1 && t->stride(0) < cols)) {
+            c.ok = false;
+            return m;
+        }
+        m.rows = (uint64_t)rows;
+        m.cols = (uint64_t)cols;
+        m.ld = rows > 1 ? (uint64_t)t->stride(0) : m.cols;
+        m.dt = c.dtype(t);
+        m.p = c.ptr<void>(t);
+        return m;
+    }
+    bool absent(int i) const { return c.ok && c.a[i] == Py_None; }
+    uint8_t* bytes(int i, uint64_t count) {
+        const at::Tensor* t = any(i);
+        if (t && (t->scalar_type() != at::kByte || !t->is_contiguous() || (uint64_t)t->numel() < count)) c.ok = false;
+        return c.ptr<uint8_t>(t);
+    }
+    // codes and scales of an 8-bit matrix
+    uint8_t* codes(int i, uint64_t rows, uint64_t cols) { return bytes(i, rows * ((cols + 127) / 128 * 128)); }
+    uint8_t* scales(int i, uint64_t rows, uint64_t cols) { return bytes(i, 4 * rows * ((cols + 511) / 512)); }
+    void* scratch(int i, uint64_t& size) {
+        size = 0;
+        if (!c.ok || c.a[i] == Py_None) return nullptr;
+        const at::Tensor* t = any(i);
+        if (t && !t->is_contiguous()) c.ok = false;
+        size = c.bytes(t);
+        return c.ptr<void>(t);
+    }
+    const void* tokens(int i, int& index, uint64_t& count) {
+        const at::Tensor* t = any(i);
+        index = THC_I32;
+        count = 0;
+        if (!c.ok || t->dim() != 1 || !t->is_contiguous() || (t->scalar_type() != at::kInt && t->scalar_type() != at::kLong)) {
+            c.ok = false;
+            return nullptr;
+        }
+        index = t->scalar_type() == at::kLong ? THC_I64 : THC_I32;
+        count = (uint64_t)t->numel();
+        return c.ptr<void>(t);
+    }
+    int format(int i) {
+        const uint64_t f = c.u64(i);
+        if (f > 1u) c.ok = false;
+        return (int)f;
+    }
+    float number(int i) {
+        if (!c.ok || !PyFloat_CheckExact(c.a[i])) {
+            c.ok = false;
+            return 0.0f;
+        }
+        return (float)PyFloat_AS_DOUBLE(c.a[i]);
+    }
+};
+
+THC_FN(fp8_quantize_) {   // x, format, q, scales, q_t, scales_t, tile, stream
+    Args c(args, n, 8);
+    Operands o(c);
+    const auto x = o.matrix(0);
+    const int format = o.format(1), tile = c.truth(6);
+    if (c.ok && (o.absent(2) != o.absent(3) || o.absent(4) != o.absent(5))) c.ok = false;
+    uint8_t *q = nullptr, *qs = nullptr, *qt = nullptr, *qts = nullptr;
+    if (c.ok && !o.absent(2)) {
+        q = o.codes(2, x.rows, x.cols);
+        qs = o.scales(3, x.rows, x.cols);
+    }
+    if (c.ok && !o.absent(4)) {
+        qt = o.codes(4, x.cols, x.rows);
+        qts = o.scales(5, x.cols, x.rows);
+    }
+    void* s = c.stream(7);
+    return finish(c, [&] {
+        return entry<decltype(thc_fp8_quantize)>(kFp8Quantize)(x.p, x.dt, x.rows, x.cols, x.ld, format, tile, q, qs, qt,
+                                                               qts, s);
+    });
+}
+THC_FN(fp8_dequantize_) {   // q, scales, format, out, stream
+    Args c(args, n, 5);
+    Operands o(c);
+    const auto out = o.matrix(3);
+    const int format = o.format(2);
+    const uint8_t* q = o.codes(0, out.rows, out.cols);
+    const uint8_t* qs = o.scales(1, out.rows, out.cols);
+    void* s = c.stream(4);
+    return finish(c, [&] {
+        return entry<decltype(thc_fp8_dequantize)>(kFp8Dequantize)(q, qs, format, out.rows, out.cols, out.dt, out.p, out.ld,
+                                                                   s);
+    });
+}
+THC_FN(fp8_matmul_) {   // a, a_scales, a_format, b, b_scales, b_format, K, c, workspace, accumulate, stream
+    Args c(args, n, 11);
+    Operands o(c);
+    const auto out = o.matrix(7);
+    const uint64_t K = c.u64(6);
+    if (K > kMost) c.ok = false;
+    const int fa = o.format(2), fb = o.format(5), add = c.truth(9);
+    const uint8_t* a = o.codes(0, out.rows, K);
+    const uint8_t* as = o.scales(1, out.rows, K);
+    const uint8_t* b = o.codes(3, out.cols, K);
+    const uint8_t* bs = o.scales(4, out.cols, K);
+    uint64_t wb;
+    void* ws = o.scratch(8, wb);
+    void* s = c.stream(10);
+    return finish(c, [&] {
+        return entry<decltype(thc_fp8_matmul)>(kFp8Matmul)(a, as, fa, b, bs, fb, out.rows, out.cols, K, add, out.dt, out.p,
+                                                           out.ld, ws, wb, s);
+    });
+}
+THC_FN(fp8_linear_) {   // x, x_format, b, b_scales, b_format, out, workspace, stream
+    Args c(args, n, 8);
+    Operands o(c);
+    const auto x = o.matrix(0), out = o.matrix(5);
+    if (x.rows != out.rows) c.ok = false;
+    const int fx = o.format(1), fb = o.format(4);
+    const uint8_t* b = o.codes(2, out.cols, x.cols);
+    const uint8_t* bs = o.scales(3, out.cols, x.cols);
+    uint64_t wb;
+    void* ws = o.scratch(6, wb);
+    void* s = c.stream(7);
+    return finish(c, [&] {
+        return entry<decltype(thc_fp8_linear)>(kFp8Linear)(x.p, x.dt, x.rows, x.cols, x.ld, fx, b, bs, fb, out.cols, out.dt,
+                                                           out.p, out.ld, ws, wb, s);
+    });
+}
+THC_FN(embed_forward_) {   // table, tokens, scale, out, stream
+    Args c(args, n, 5);
+    Operands o(c);
+    const auto table = o.matrix(0), out = o.matrix(3);
+    int index;
+    uint64_t count;
+    const void* tokens = o.tokens(1, index, count);
+    if (out.rows != count || out.cols != table.cols) c.ok = false;
+    const float scale = o.number(2);
+    void* s = c.stream(4);
+    return finish(c, [&] {
+        return entry<decltype(thc_embed_forward)>(kEmbedForward)(table.p, table.dt, table.rows, table.cols, table.ld, tokens,
+                                                                 index, count, scale, out.dt, out.p, out.ld, s);
+    });
+}
+THC_FN(embed_backward_) {   // grad_out, tokens, scale, grad_table, workspace, accumulate, stream
+    Args c(args, n, 7);
+    Operands o(c);
+    const auto g = o.matrix(0), table = o.matrix(3);
+    int index;
+    uint64_t count;
+    const void* tokens = o.tokens(1, index, count);
+    if (g.rows != count || g.cols != table.cols) c.ok = false;
+    const float scale = o.number(2);
+    uint64_t wb;
+    void* ws = o.scratch(4, wb);
+    const int add = c.truth(5);
+    void* s = c.stream(6);
+    return finish(c, [&] {
+        return entry<decltype(thc_embed_backward)>(kEmbedBackward)(g.p, g.dt, g.ld, tokens, index, count, table.rows,
+                                                                   table.cols, scale, add, table.dt, table.p, table.ld, ws,
+                                                                   wb, s);
+    });
+}
+
 // bind(name, address): where the loaded library's entry point is.
 PyObject* bind(PyObject*, PyObject* args) {
     const char* name;
@@ -606,6 +796,12 @@ PyMethodDef kMethods[] = {
     THC_METHOD("topkc_select", topkc_select_),
     THC_METHOD("topkc_gather_sum", topkc_gather_sum_),
     THC_METHOD("topkc_scatter_mean", topkc_scatter_mean_),
+    THC_METHOD("thc_fp8_quantize", fp8_quantize_),
+    THC_METHOD("thc_fp8_dequantize", fp8_dequantize_),
+    THC_METHOD("thc_fp8_matmul", fp8_matmul_),
+    THC_METHOD("thc_fp8_linear", fp8_linear_),
+    THC_METHOD("thc_embed_forward", embed_forward_),
+    THC_METHOD("thc_embed_backward", embed_backward_),
     {"bind", bind, METH_VARARGS, nullptr},
     {"names", names, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};

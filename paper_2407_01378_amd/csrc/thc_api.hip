@@ -1114,4 +1114,203 @@ int thc_aggregate_decode_minmax(const uint8_t* const* payloads, uint32_t W, cons
     return finish(thc::launch_aggregate_decode_ranged(a, ptrs, bits, st));
 }
 
+/* ---- 8-bit matrices with a scale per block of 128, and the embedding ---------------------- */
+static constexpr uint64_t kMaxRows = 0x7FFFFFFFull;        // rows, free columns, tokens
+static constexpr uint64_t kMaxContracted = 1ull << 22;     // columns of an 8-bit matrix: 256 rows of codes stay below 2^31 bytes
+
+static int check_fp8_format(int format) {
+    return (format == THC_E4M3 || format == THC_E5M2) ? THC_OK : THC_ERR_DTYPE;
+}
+static uintptr_t dtype_bytes(int dt) { return dt == THC_F32 ? 4 : 2; }
+static uint64_t round16(uint64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+uint64_t thc_fp8_row_bytes(uint64_t cols) { return cols > kMaxContracted ? 0 : thc::fp8_row_bytes(cols); }
+
+uint64_t thc_fp8_scale_bytes(uint64_t rows, uint64_t cols) {
+    return rows > kMaxRows || cols > kMaxContracted ? 0 : 4 * thc::fp8_scale_words(rows, cols);
+}
+
+int thc_fp8_quantize(const void* x, thc_dtype dt, uint64_t rows, uint64_t cols, uint64_t ld, int format, int tile,
+                     uint8_t* q, uint8_t* scales, uint8_t* q_t, uint8_t* scales_t, void* stream) {
+    int rc = check_dtype(dt);
+    if (rc == THC_OK) rc = check_fp8_format(format);
+    if (rc != THC_OK) return rc;
+    if (rows > kMaxRows || cols > kMaxRows) return THC_ERR_SIZE;
+    if (rows == 0 || cols == 0) return THC_OK;
+    if (!x || !q != !scales || !q_t != !scales_t || (!q && !q_t)) return THC_ERR_NULL;
+    if ((q && cols > kMaxContracted) || (q_t && rows > kMaxContracted) || ld < cols || ld > kMaxCoords) return THC_ERR_SIZE;
+    if (!aligned(x, dtype_bytes(dt)) || !aligned(q, 16) || !aligned(scales, 16) || !aligned(q_t, 16) ||
+        !aligned(scales_t, 16))
+        return THC_ERR_ALIGN;
+    thc::Fp8QuantizeArgs a{};
+    a.x = x;
+    a.ld = ld;
+    a.rows = (uint32_t)rows;
+    a.cols = (uint32_t)cols;
+    a.q = q;
+    a.scales = reinterpret_cast<uint32_t*>(scales);
+    a.q_t = q_t;
+    a.scales_t = reinterpret_cast<uint32_t*>(scales_t);
+    return finish(thc::launch_fp8_quantize(a, dt == THC_BF16, format == THC_E5M2, tile != 0,
+                                           static_cast<hipStream_t>(stream)));
+}
+
+int thc_fp8_dequantize(const uint8_t* q, const uint8_t* scales, int format, uint64_t rows, uint64_t cols,
+                       thc_dtype out_dt, void* out, uint64_t ld, void* stream) {
+    int rc = check_fp8_format(format);
+    if (rc == THC_OK) rc = check_dtype(out_dt);
+    if (rc != THC_OK) return rc;
+    if (rows > kMaxRows || cols > kMaxContracted) return THC_ERR_SIZE;
+    if (rows == 0 || cols == 0) return THC_OK;
+    if (!q || !scales || !out) return THC_ERR_NULL;
+    if (ld < cols || ld > kMaxCoords) return THC_ERR_SIZE;
+    if (!aligned(q, 16) || !aligned(scales, 16) || !aligned(out, dtype_bytes(out_dt))) return THC_ERR_ALIGN;
+    return finish(thc::launch_fp8_dequantize(q, reinterpret_cast<const uint32_t*>(scales), format == THC_E5M2,
+                                             (uint32_t)rows, (uint32_t)cols, out_dt == THC_BF16, out, ld,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+static bool fp8_product_in_range(uint64_t M, uint64_t N, uint64_t K) {
+    return M <= kMaxRows && N <= kMaxRows && K <= kMaxContracted;
+}
+
+uint64_t thc_fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
+    return fp8_product_in_range(M, N, K) ? thc::fp8_matmul_workspace_bytes(M, N, K) : 0;
+}
+
+int thc_fp8_matmul(const uint8_t* a, const uint8_t* a_scales, int a_format, const uint8_t* b, const uint8_t* b_scales,
+                   int b_format, uint64_t M, uint64_t N, uint64_t K, int accumulate, thc_dtype out_dt, void* c,
+                   uint64_t ldc, void* workspace, uint64_t workspace_bytes, void* stream) {
+    int rc = check_fp8_format(a_format);
+    if (rc == THC_OK) rc = check_fp8_format(b_format);
+    if (rc == THC_OK) rc = check_dtype(out_dt);
+    if (rc != THC_OK) return rc;
+    if (!fp8_product_in_range(M, N, K)) return THC_ERR_SIZE;
+    if (M == 0 || N == 0) return THC_OK;
+    const uint64_t need = thc::fp8_matmul_workspace_bytes(M, N, K);
+    if (!c || (K != 0 && (!a || !a_scales || !b || !b_scales)) || (need != 0 && !workspace)) return THC_ERR_NULL;
+    if (ldc < N || ldc > kMaxCoords || workspace_bytes < need) return THC_ERR_SIZE;
+    if (!aligned(a, 16) || !aligned(a_scales, 16) || !aligned(b, 16) || !aligned(b_scales, 16) ||
+        !aligned(c, dtype_bytes(out_dt)) || (need != 0 && !aligned(workspace, 16)))
+        return THC_ERR_ALIGN;
+    thc::Fp8MatmulArgs m{};
+    m.a = a;
+    m.a_scales = reinterpret_cast<const uint32_t*>(a_scales);
+    m.b = b;
+    m.b_scales = reinterpret_cast<const uint32_t*>(b_scales);
+    m.M = (uint32_t)M;
+    m.N = (uint32_t)N;
+    m.K = (uint32_t)K;
+    m.a_e5m2 = a_format == THC_E5M2;
+    m.b_e5m2 = b_format == THC_E5M2;
+    m.accumulate = accumulate != 0;
+    m.out_bf16 = out_dt == THC_BF16;
+    m.c = c;
+    m.ldc = ldc;
+    m.workspace = static_cast<float*>(workspace);
+    return finish(thc::launch_fp8_matmul(m, static_cast<hipStream_t>(stream)));
+}
+
+// The workspace of thc_fp8_linear: the codes of x, its scales, the product's own workspace.
+uint64_t thc_fp8_linear_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
+    if (!fp8_product_in_range(M, N, K) || M == 0 || N == 0) return 0;
+    return M * thc::fp8_row_bytes(K) + round16(4 * thc::fp8_scale_words(M, K)) + thc::fp8_matmul_workspace_bytes(M, N, K);
+}
+
+int thc_fp8_linear(const void* x, thc_dtype dt, uint64_t M, uint64_t K, uint64_t ldx, int x_format, const uint8_t* b,
+                   const uint8_t* b_scales, int b_format, uint64_t N, thc_dtype out_dt, void* out, uint64_t ldo,
+                   void* workspace, uint64_t workspace_bytes, void* stream) {
+    int rc = check_dtype(dt);
+    if (rc == THC_OK) rc = check_fp8_format(x_format);
+    if (rc == THC_OK) rc = check_fp8_format(b_format);
+    if (rc == THC_OK) rc = check_dtype(out_dt);
+    if (rc != THC_OK) return rc;
+    if (!fp8_product_in_range(M, N, K)) return THC_ERR_SIZE;
+    if (M == 0 || N == 0) return THC_OK;
+    const uint64_t need = thc_fp8_linear_workspace_bytes(M, N, K);
+    if (!out || (K != 0 && (!x || !b || !b_scales)) || (need != 0 && !workspace)) return THC_ERR_NULL;
+    if (ldx < K || ldx > kMaxCoords || ldo < N || ldo > kMaxCoords || workspace_bytes < need) return THC_ERR_SIZE;
+    if (!aligned(x, dtype_bytes(dt)) || !aligned(b, 16) || !aligned(b_scales, 16) || !aligned(out, dtype_bytes(out_dt)) ||
+        (need != 0 && !aligned(workspace, 16)))
+        return THC_ERR_ALIGN;
+    uint8_t* codes = static_cast<uint8_t*>(workspace);
+    uint8_t* scales = codes + M * thc::fp8_row_bytes(K);
+    const uint64_t used = M * thc::fp8_row_bytes(K) + round16(4 * thc::fp8_scale_words(M, K));
+    rc = thc_fp8_quantize(x, dt, M, K, ldx, x_format, 0, codes, scales, nullptr, nullptr, stream);
+    if (rc != THC_OK) return rc;
+    return thc_fp8_matmul(codes, scales, x_format, b, b_scales, b_format, M, N, K, 0, out_dt, out, ldo, codes + used,
+                          workspace_bytes - used, stream);
+}
+
+static int check_index(int index) { return (index == THC_I32 || index == THC_I64) ? THC_OK : THC_ERR_DTYPE; }
+
+int thc_embed_forward(const void* table, thc_dtype dt, uint64_t vocab, uint64_t dim, uint64_t ld, const void* tokens,
+                      int index, uint64_t count, float scale, thc_dtype out_dt, void* out, uint64_t ldo, void* stream) {
+    int rc = check_dtype(dt);
+    if (rc == THC_OK) rc = check_dtype(out_dt);
+    if (rc == THC_OK) rc = check_index(index);
+    if (rc != THC_OK) return rc;
+    if (vocab > kMaxRows || dim > kMaxRows || count > kMaxRows) return THC_ERR_SIZE;
+    if (count == 0 || dim == 0) return THC_OK;
+    if ((!table && vocab != 0) || !tokens || !out) return THC_ERR_NULL;
+    if (ld < dim || ld > kMaxCoords || ldo < dim || ldo > kMaxCoords) return THC_ERR_SIZE;
+    if (!aligned(table, dtype_bytes(dt)) || !aligned(tokens, index == THC_I64 ? 8 : 4) || !aligned(out, dtype_bytes(out_dt)))
+        return THC_ERR_ALIGN;
+    thc::EmbedArgs a{};
+    a.in = table;
+    a.ld_in = ld;
+    a.out = out;
+    a.ld_out = ldo;
+    a.tokens = tokens;
+    a.count = (uint32_t)count;
+    a.vocab = (uint32_t)vocab;
+    a.dim = (uint32_t)dim;
+    a.wide_tokens = index == THC_I64;
+    a.in_bf16 = dt == THC_BF16;
+    a.out_bf16 = out_dt == THC_BF16;
+    a.scale = scale;
+    return finish(thc::launch_embed_forward(a, static_cast<hipStream_t>(stream)));
+}
+
+static bool embed_gradient_in_range(uint64_t count, uint64_t vocab, uint64_t dim) {
+    return count <= kMaxRows && vocab <= kMaxRows && dim <= kMaxRows && count * dim < kMaxCoords;
+}
+
+uint64_t thc_embed_backward_workspace_bytes(uint64_t count, uint64_t vocab, uint64_t dim) {
+    return embed_gradient_in_range(count, vocab, dim) ? thc::embed_backward_workspace_bytes(count, vocab, dim) : 0;
+}
+
+int thc_embed_backward(const void* grad_out, thc_dtype dt, uint64_t ld, const void* tokens, int index, uint64_t count,
+                       uint64_t vocab, uint64_t dim, float scale, int accumulate, thc_dtype out_dt, void* grad_table,
+                       uint64_t ldt, void* workspace, uint64_t workspace_bytes, void* stream) {
+    int rc = check_dtype(dt);
+    if (rc == THC_OK) rc = check_dtype(out_dt);
+    if (rc == THC_OK) rc = check_index(index);
+    if (rc != THC_OK) return rc;
+    if (!embed_gradient_in_range(count, vocab, dim)) return THC_ERR_SIZE;
+    if (vocab == 0 || dim == 0 || (count == 0 && accumulate)) return THC_OK;
+    const uint64_t need = thc::embed_backward_workspace_bytes(count, vocab, dim);
+    if (!grad_table || (count != 0 && (!grad_out || !tokens)) || (need != 0 && !workspace)) return THC_ERR_NULL;
+    if (ld < dim || ld > kMaxCoords || ldt < dim || ldt > kMaxCoords || workspace_bytes < need) return THC_ERR_SIZE;
+    if (!aligned(grad_out, dtype_bytes(dt)) || !aligned(tokens, index == THC_I64 ? 8 : 4) ||
+        !aligned(grad_table, dtype_bytes(out_dt)) || (need != 0 && !aligned(workspace, 16)))
+        return THC_ERR_ALIGN;
+    thc::EmbedArgs a{};
+    a.in = grad_out;
+    a.ld_in = ld;
+    a.out = grad_table;
+    a.ld_out = ldt;
+    a.tokens = tokens;
+    a.count = (uint32_t)count;
+    a.vocab = (uint32_t)vocab;
+    a.dim = (uint32_t)dim;
+    a.wide_tokens = index == THC_I64;
+    a.in_bf16 = dt == THC_BF16;
+    a.out_bf16 = out_dt == THC_BF16;
+    a.accumulate = accumulate != 0;
+    a.scale = scale;
+    a.workspace = static_cast<uint32_t*>(workspace);
+    return finish(thc::launch_embed_backward(a, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

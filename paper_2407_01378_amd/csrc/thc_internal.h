@@ -228,6 +228,52 @@ hipError_t launch_topkc_gather_sum(const FusedWorkerPtrs& ptrs, bool bf16, uint3
 hipError_t launch_topkc_scatter(const uint16_t* values, const uint32_t* indices, uint32_t J, uint32_t C,
                                 uint32_t W, uint64_t n, float* out, hipStream_t stream);
 
+// ---- 8-bit matrices with a scale per block of 128 (thc_fp8_quantize.hip, thc_fp8_matmul.hip) -------
+constexpr uint64_t kFp8Block = 128;
+inline uint64_t fp8_row_bytes(uint64_t cols) { return (cols + kFp8Block - 1) / kFp8Block * kFp8Block; }
+inline uint64_t fp8_scale_words(uint64_t rows, uint64_t cols) { return (cols + 4 * kFp8Block - 1) / (4 * kFp8Block) * rows; }
+struct Fp8QuantizeArgs {
+    const void* x;
+    uint64_t ld;
+    uint32_t rows, cols;
+    uint8_t* q;           // rows x cols, or null
+    uint32_t* scales;
+    uint8_t* q_t;         // cols x rows, or null
+    uint32_t* scales_t;
+};
+hipError_t launch_fp8_quantize(const Fp8QuantizeArgs& a, bool bf16, bool e5m2, bool tile, hipStream_t stream);
+hipError_t launch_fp8_dequantize(const uint8_t* q, const uint32_t* scales, bool e5m2, uint32_t rows, uint32_t cols,
+                                 bool out_bf16, void* out, uint64_t ld, hipStream_t stream);
+struct Fp8MatmulArgs {
+    const uint8_t* a;     // M x K
+    const uint32_t* a_scales;
+    const uint8_t* b;     // N x K
+    const uint32_t* b_scales;
+    uint32_t M, N, K;
+    uint32_t a_e5m2, b_e5m2, accumulate, out_bf16;
+    void* c;
+    uint64_t ldc;
+    float* workspace;
+};
+uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
+hipError_t launch_fp8_matmul(const Fp8MatmulArgs& a, hipStream_t stream);
+
+// ---- embedding (thc_embed.hip) -----------------------------------------------------------------
+struct EmbedArgs {
+    const void* in;       // forward: table; backward: grad_out
+    uint64_t ld_in;
+    void* out;            // forward: rows of the tokens; backward: grad_table
+    uint64_t ld_out;
+    const void* tokens;
+    uint32_t count, vocab, dim;
+    uint32_t wide_tokens, in_bf16, out_bf16, accumulate;
+    float scale;
+    uint32_t* workspace;  // backward
+};
+hipError_t launch_embed_forward(const EmbedArgs& a, hipStream_t stream);
+uint64_t embed_backward_workspace_bytes(uint64_t count, uint64_t vocab, uint64_t dim);
+hipError_t launch_embed_backward(const EmbedArgs& a, hipStream_t stream);
+
 constexpr int kMaxAggBatch = 16;
 struct PayloadBatch {
     const uint8_t* p[kMaxAggBatch];

@@ -1,0 +1,379 @@
+"""8-bit matrices on the GPU against the 64-bit oracle: codes and scales exactly, products within the bound of
+their fp32 sums, and exactly where every partial sum is a whole number below 2^24."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2407_01378_amd as thc
+from oracle import fp8 as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+CODE = {"e4m3": thc.THC_E4M3, "e5m2": thc.THC_E5M2}
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _buffers(rows, cols, fill=0xAB):
+    return (torch.full((rows * thc.thc_fp8_row_bytes(cols),), fill, dtype=torch.uint8, device=DEV),
+            torch.full((thc.thc_fp8_scale_bytes(rows, cols),), fill, dtype=torch.uint8, device=DEV))
+
+
+def _matrix(rows, cols, dt, seed, pitch=None, shift=0):
+    """Values over many magnitudes, and blocks at the edges of the formats' ranges."""
+    g = _gen(seed)
+    x = torch.randn(rows, cols, generator=g, device=DEV) * torch.exp(4 * torch.randn(rows, cols, generator=g, device=DEV))
+    if rows > 2:
+        x[rows // 2] = 0.0
+        x[0] *= 2.0 ** -110
+        x[rows - 1] *= 2.0 ** 90
+        x[1, ::3] = -0.0
+    whole = torch.full((rows * (pitch or cols) + shift,), float("nan"), dtype=DT[dt], device=DEV)[shift:]
+    v = whole.as_strided((rows, cols), (pitch or cols, 1))
+    v.copy_(x)
+    return v
+
+
+def _quantize(x, fmt, tile, both):
+    rows, cols = x.shape
+    q, s = _buffers(rows, cols)
+    qt, st = _buffers(cols, rows) if both else (None, None)
+    thc.thc_fp8_quantize(x, CODE[fmt], q, s, qt, st, tile)
+    torch.cuda.synchronize()
+    return q, s, qt, st
+
+
+def _check_codes(x64, fmt, tile, q, s):
+    codes, scales = O.quantize(x64, fmt, tile)
+    assert np.array_equal(s.cpu().numpy(), O.pack_scales(scales))
+    assert np.array_equal(q.cpu().numpy().reshape(codes.shape), codes)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("tile", [False, True])
+@pytest.mark.parametrize("rows,cols,pitch,shift", [
+    (1, 1, None, 0), (1, 128, None, 0), (3, 129, None, 0), (128, 128, None, 0), (130, 515, 520, 0), (257, 640, 641, 1),
+    (64, 1000, 1024, 0), (5, 7, 9, 3), (200, 24, 24, 0)])
+def test_quantize(fmt, dt, tile, rows, cols, pitch, shift):
+    x = _matrix(rows, cols, dt, rows + cols, pitch, shift)
+    x64 = x.double().cpu().numpy()
+    q, s, qt, st = _quantize(x, fmt, tile, True)
+    _check_codes(x64, fmt, tile, q, s)
+    _check_codes(np.ascontiguousarray(x64.T), fmt, tile, qt, st)
+    q1, s1, _, _ = _quantize(x, fmt, tile, False)
+    assert torch.equal(q1, q) and torch.equal(s1, s)
+    qt1, st1 = _buffers(cols, rows)
+    thc.thc_fp8_quantize(x, CODE[fmt], None, None, qt1, st1, tile)
+    assert torch.equal(qt1, qt) and torch.equal(st1, st)
+    for out_dt in ("f32", "bf16"):
+        for p in (cols, cols + 5):
+            out = torch.full((rows, p), 7.0, dtype=DT[out_dt], device=DEV)
+            thc.thc_fp8_dequantize(q, s, CODE[fmt], out[:, :cols])
+            want = torch.tensor(O.values(*O.quantize(x64, fmt, tile), fmt, cols)).float().to(DT[out_dt])
+            assert torch.equal(out[:, :cols].cpu(), want)
+            assert (out[:, cols:] == 7.0).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_every_value_between_two_codes(fmt):
+    """A block whose scale is 1: every code, every midpoint and its neighbours in fp32."""
+    v = O.code_values(fmt)[:0x80]
+    v = v[np.isfinite(v)].astype(np.float32)
+    mid = ((v[1:].astype(np.float64) + v[:-1]) / 2).astype(np.float32)
+    x = np.concatenate([v, mid, np.nextafter(mid, np.float32(np.inf)), np.nextafter(mid, np.float32(0))])
+    x = np.concatenate([x, -x])
+    x = np.concatenate([x, np.zeros(-x.size % 127, np.float32)]).reshape(-1, 127)
+    x = np.concatenate([np.full((x.shape[0], 1), O.FORMATS[fmt][2], np.float32), x], axis=1)
+    q, s, qt, st = _quantize(torch.tensor(x, device=DEV), fmt, False, True)
+    assert (s.cpu().numpy().reshape(-1, 4)[:, 0] == 127).all()
+    _check_codes(x.astype(np.float64), fmt, False, q, s)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_values_that_are_not_finite(fmt, dt):
+    x = _matrix(140, 300, dt, 5)
+    x[3, 7], x[70, 200], x[139, 299] = float("nan"), float("inf"), -float("inf")
+    x64 = x.double().cpu().numpy()
+    for tile in (False, True):
+        q, s, qt, st = _quantize(x, fmt, tile, True)
+        _check_codes(x64, fmt, tile, q, s)
+        _check_codes(np.ascontiguousarray(x64.T), fmt, tile, qt, st)
+        out = torch.empty(140, 300, device=DEV)
+        thc.thc_fp8_dequantize(q, s, CODE[fmt], out)
+        want = O.values(*O.quantize(x64, fmt, tile), fmt, 300)
+        assert np.array_equal(out.cpu().numpy(), want.astype(np.float32), equal_nan=True)
+
+
+# -------------------------------------------------------------------------------- products
+SHAPES = [  # tokens from one to many, odd sizes, blocks that do not fill a word of scales
+    (1, 1, 1), (1, 16, 128), (1, 2048, 640), (2, 33, 515), (3, 17, 1000), (5, 300, 2048), (16, 256, 512), (17, 129, 300),
+    (24, 512, 1100), (33, 64, 4096), (40, 200, 130), (64, 1000, 384), (65, 257, 900), (100, 1, 5000), (128, 128, 128), (129, 130, 131),
+    (250, 515, 1025), (256, 256, 256), (257, 511, 640), (300, 700, 2200), (513, 260, 96), (1000, 77, 3000), (16, 16, 40000),
+    (512, 768, 1536)]
+
+
+def _whole(rows, cols, fmt, seed):
+    """Codes of small whole numbers and scales of 1, 2 and 4: every product and partial sum is a whole number."""
+    rng = np.random.default_rng(seed)
+    v = rng.integers(-2, 3, (rows, cols)).astype(np.float64)
+    C = thc.thc_fp8_row_bytes(cols)
+    codes = np.zeros((rows, C), dtype=np.uint8)
+    values = O.code_values(fmt)
+    for k in range(-2, 3):
+        codes[:, :cols][v == k] = int(np.flatnonzero(values == k)[0])
+    scales = rng.integers(127, 130, (rows, C // 128)).astype(np.uint8)
+    exact = v * np.repeat(2.0 ** (scales.astype(float) - 127), 128, axis=1)[:, :cols]
+    return (torch.tensor(codes.reshape(-1), device=DEV), torch.tensor(O.pack_scales(scales), device=DEV),
+            torch.tensor(exact, device=DEV))
+
+
+def _ws(bytes_):
+    return torch.full((bytes_,), 0xCD, dtype=torch.uint8, device=DEV) if bytes_ else None
+
+
+def _matmul(a, fa, b, fb, K, c, accumulate=False):
+    M, N = c.shape
+    return thc.thc_fp8_matmul(a[0], a[1], CODE[fa], b[0], b[1], CODE[fb], K, c,
+                              _ws(thc.thc_fp8_matmul_workspace_bytes(M, N, K)), accumulate)
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_products_of_whole_numbers_are_exact(M, N, K):
+    for i, (fa, fb) in enumerate([("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e5m2")]):
+        a, b = _whole(M, K, fa, 10 + i), _whole(N, K, fb, 20 + i)
+        want = a[2] @ b[2].t()
+        assert float((a[2].abs() @ b[2].abs().t()).max()) < 2 ** 24
+        whole = torch.full((M, N + 3), float("nan"), device=DEV)
+        _matmul(a, fa, b, fb, K, whole[:, :N])
+        assert torch.equal(whole[:, :N].double(), want) and whole[:, N:].isnan().all()
+        packed = torch.full((M, N), float("nan"), device=DEV)
+        _matmul(a, fa, b, fb, K, packed)
+        assert torch.equal(packed.double(), want)
+        _matmul(a, fa, b, fb, K, packed, accumulate=True)
+        assert torch.equal(packed.double(), 2 * want)
+        half = torch.full((M, N), float("nan"), dtype=torch.bfloat16, device=DEV)
+        _matmul(a, fa, b, fb, K, half)
+        assert torch.equal(half, want.float().bfloat16())
+        start = half.clone()
+        _matmul(a, fa, b, fb, K, half, accumulate=True)
+        assert torch.equal(half, (start.float() + want.float()).bfloat16())
+        wide = torch.full((M, N + 1), 5.0, dtype=torch.bfloat16, device=DEV)
+        _matmul(a, fa, b, fb, K, wide[:, :N])
+        assert torch.equal(wide[:, :N], want.float().bfloat16()) and (wide[:, N] == 5.0).all()
+
+
+def _sum_bound(size, K):
+    """fp32 results: products are exact in fp32; each of the K additions is off by at most 2^-23 of a partial sum (2^-24 were it
+    rounded to nearest; the matrix unit may cut off), and no partial sum exceeds the sum of magnitudes."""
+    return size * K * 2.0 ** -23 + 1e-38
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 300, 2048), (7, 64, 1000), (31, 130, 4000), (200, 300, 700), (300, 513, 1300)])
+def test_products_of_quantized_values(M, N, K):
+    for fa in ("e4m3", "e5m2"):
+        x, w = _matrix(M, K, "bf16", M), _matrix(N, K, "f32", N)
+        if M > 2:
+            x[M - 1] *= 2.0 ** -80       # (2^90 times 2^90 is beyond fp32)
+        w[N - 1] *= 2.0 ** -80
+        qa, qb = _quantize(x, fa, False, False), _quantize(w, "e4m3", True, False)
+        A = torch.tensor(O.values(*O.quantize(x.double().cpu().numpy(), fa, False), fa, K), device=DEV)
+        B = torch.tensor(O.values(*O.quantize(w.double().cpu().numpy(), "e4m3", True), "e4m3", K), device=DEV)
+        want, size = A @ B.t(), A.abs() @ B.abs().t()
+        c = torch.empty(M, N, device=DEV)
+        _matmul(qa, fa, qb, "e4m3", K, c)
+        assert ((c.double() - want).abs() <= _sum_bound(size, K)).all()
+        # bf16: of every 8 products at most 7 are cut, each by less than 2^-13 of the largest
+        half = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+        _matmul(qa, fa, qb, "e4m3", K, half)
+        cut = 7 * 2.0 ** -13 * size
+        assert ((half.double() - want).abs() <= cut + _sum_bound(size, K) + 2.0 ** -8 * (want.abs() + cut)).all()
+        # a layer: the same bits as the quantizer and the product by themselves
+        for out_dt in ("f32", "bf16"):
+            y, z = torch.empty(M, N, dtype=DT[out_dt], device=DEV), torch.empty(M, N, dtype=DT[out_dt], device=DEV)
+            thc.thc_fp8_linear(x, CODE[fa], qb[0], qb[1], thc.THC_E4M3, y, _ws(thc.thc_fp8_linear_workspace_bytes(M, N, K)))
+            _matmul(qa, fa, qb, "e4m3", K, z)
+            assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_linear_is_quantize_and_product(M, N, K, dt):
+    """Also for rows that are not on the 16-byte grid."""
+    b = _whole(N, K, "e4m3", 3)
+    for shift, pitch in ((0, K), (0, (K + 15) // 16 * 16), (1, K + 1)):
+        x = _matrix(M, K, dt, 7, pitch, shift)
+        qa = _quantize(x, "e5m2", False, False)
+        y, z = torch.empty(M, N, device=DEV), torch.empty(M, N, device=DEV)
+        thc.thc_fp8_linear(x, thc.THC_E5M2, b[0], b[1], thc.THC_E4M3, y, _ws(thc.thc_fp8_linear_workspace_bytes(M, N, K)))
+        _matmul(qa, "e5m2", b, "e4m3", K, z)
+        assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("M", [1, 20, 300])
+def test_nan_reaches_its_row_and_no_other(M):
+    N, K = 200, 700
+    x = torch.randn(M, K, generator=_gen(1), device=DEV)
+    w = torch.randn(N, K, generator=_gen(2), device=DEV)
+    x[M // 2, 650] = float("inf")
+    w[77, 3] = float("nan")
+    qb = _quantize(w, "e4m3", False, False)
+    y = torch.empty(M, N, device=DEV)
+    thc.thc_fp8_linear(x, thc.THC_E4M3, qb[0], qb[1], thc.THC_E4M3, y, _ws(thc.thc_fp8_linear_workspace_bytes(M, N, K)))
+    want = torch.zeros(M, N, dtype=torch.bool, device=DEV)
+    want[M // 2], want[:, 77] = True, True
+    assert torch.equal(y.isnan(), want)
+
+
+@pytest.mark.parametrize("M,N", [(1, 5), (300, 40)])
+def test_empty_sum(M, N):
+    e = torch.empty(0, dtype=torch.uint8, device=DEV)
+    c = torch.full((M, N + 1), 3.0, device=DEV)
+    thc.thc_fp8_matmul(e, e, 0, e, e, 0, 0, c[:, :N], None, accumulate=True)
+    assert (c == 3.0).all()
+    thc.thc_fp8_matmul(e, e, 0, e, e, 0, 0, c[:, :N], None)
+    assert (c[:, :N] == 0.0).all() and (c[:, N] == 3.0).all()
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_extreme_scales(out):
+    """Products of small and large blocks: scales at both ends (bf16 results), or as far as the values are normal
+    fp32 numbers (fp32 results)."""
+    small, large = (10, 244) if out == "f32" else (0, 254)
+    for M in (3, 260):
+        N, K = 300, 256
+        a, b = _whole(M, K, "e4m3", 1), _whole(N, K, "e4m3", 2)
+        one_a = a[2] / torch.tensor(np.repeat(2.0 ** (_unpack(a[1], M, 2) - 127.0), 128, 1), device=DEV)
+        one_b = b[2] / torch.tensor(np.repeat(2.0 ** (_unpack(b[1], N, 2) - 127.0), 128, 1), device=DEV)
+        sa = np.array([small, 200], dtype=np.uint8)[np.arange(M * 2) % 2].reshape(M, 2)
+        sb = np.array([large, 40], dtype=np.uint8)[np.arange(N * 2) % 2].reshape(N, 2)
+        fa = torch.tensor(np.repeat(2.0 ** (sa.astype(float) - 127), 128, 1), device=DEV)
+        fb = torch.tensor(np.repeat(2.0 ** (sb.astype(float) - 127), 128, 1), device=DEV)
+        want = (one_a * fa) @ (one_b * fb).t()
+        # block 0 contributes whole numbers of up to 512, block 1 whole multiples of 2^-14 of up to 2^-5: exact in fp32
+        assert torch.equal(want.float().double(), want)
+        c = torch.empty(M, N, dtype=DT[out], device=DEV)
+        _matmul((a[0], torch.tensor(O.pack_scales(sa), device=DEV)), "e4m3",
+                (b[0], torch.tensor(O.pack_scales(sb), device=DEV)), "e4m3", K, c)
+        assert torch.equal(c, want.float().to(DT[out]))
+
+
+def _unpack(packed, rows, blocks):
+    return packed.cpu().numpy().reshape(-1, rows, 4).transpose(1, 0, 2).reshape(rows, -1)[:, :blocks].astype(float)
+
+
+def test_results_are_the_same_on_every_run_and_stream():
+    M, N, K = 300, 520, 9000
+    x, w = _matrix(M, K, "bf16", 1), torch.randn(N, K, generator=_gen(9), device=DEV)
+    qb = _quantize(w, "e4m3", True, False)
+    ys = []
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(6):
+        y = torch.empty(M, N, device=DEV)
+        ws = _ws(thc.thc_fp8_linear_workspace_bytes(M, N, K))
+        torch.cuda.synchronize()
+        thc.thc_fp8_linear(x, thc.THC_E4M3, qb[0], qb[1], thc.THC_E4M3, y, ws, stream=side if i % 2 else None)
+        torch.cuda.synchronize()
+        ys.append(y)
+    assert all(torch.equal(y.view(torch.int32), ys[0].view(torch.int32)) for y in ys)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 700, 900), (20, 300, 4100), (300, 300, 8192)])
+def test_captured_and_replayed(M, N, K):
+    """A layer forward and its weight gradient in a graph, replayed on other inputs with eager work between."""
+    w = torch.randn(N, K, generator=_gen(4), device=DEV)
+    qb = _quantize(w, "e4m3", True, False)
+    x, y, dw = torch.empty(M, K, device=DEV), torch.empty(M, N, device=DEV), torch.zeros(N, K, device=DEV)
+    ws = _ws(thc.thc_fp8_linear_workspace_bytes(M, N, K))
+    wsg = _ws(thc.thc_fp8_matmul_workspace_bytes(N, K, M))
+    xt, yt = _buffers(K, M), _buffers(N, M)
+
+    def step():
+        thc.thc_fp8_linear(x, thc.THC_E4M3, qb[0], qb[1], thc.THC_E4M3, y, ws)
+        thc.thc_fp8_quantize(x, thc.THC_E4M3, None, None, xt[0], xt[1])
+        thc.thc_fp8_quantize(y, thc.THC_E5M2, None, None, yt[0], yt[1])
+        thc.thc_fp8_matmul(yt[0], yt[1], thc.THC_E5M2, xt[0], xt[1], thc.THC_E4M3, M, dw, wsg, True)
+
+    x.copy_(torch.randn(M, K, generator=_gen(0), device=DEV))
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        x.copy_(torch.randn(M, K, generator=_gen(i), device=DEV))
+        dw.fill_(float(i))
+        step()
+        torch.cuda.synchronize()
+        eager = (y.clone(), dw.clone())
+        y.zero_()
+        dw.fill_(float(i))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager[0]) and torch.equal(dw, eager[1])
+
+
+def test_gradients_against_differences():
+    """With values that 8 bits hold exactly the layer is bilinear: its gradients equal differences of the loss."""
+    T, K, N = 5, 130, 20
+    rng = np.random.default_rng(2)
+    x, w, dy = (torch.tensor(rng.integers(-3, 4, s).astype(np.float32), device=DEV) for s in ((T, K), (N, K), (T, N)))
+
+    def forward(x, w):
+        qb = _quantize(w, "e4m3", False, False)
+        y = torch.empty(T, N, device=DEV)
+        return thc.thc_fp8_linear(x, thc.THC_E4M3, qb[0], qb[1], thc.THC_E4M3, y, _ws(thc.thc_fp8_linear_workspace_bytes(T, N, K)))
+
+    wt = _quantize(w, "e4m3", False, True)[2:]
+    xt = _quantize(x, "e4m3", False, True)[2:]
+    g, gs, gt, gts = _quantize(dy, "e5m2", False, True)
+    dx, dw = torch.empty(T, K, device=DEV), torch.empty(N, K, device=DEV)
+    _matmul((g, gs), "e5m2", wt, "e4m3", N, dx)
+    _matmul((gt, gts), "e5m2", xt, "e4m3", T, dw)
+    loss = lambda x, w: float((forward(x, w).double() * dy.double()).sum())   # noqa: E731
+    for i, j in ((0, 0), (4, 129), (2, 64)):
+        e = torch.zeros_like(x)
+        e[i, j] = 1.0
+        assert (loss(x + e, w) - loss(x - e, w)) / 2 == float(dx[i, j])
+    for i, j in ((0, 0), (19, 129), (7, 127)):
+        e = torch.zeros_like(w)
+        e[i, j] = 1.0
+        assert (loss(x, w + e) - loss(x, w - e)) / 2 == float(dw[i, j])
+
+
+def test_rows_far_apart():
+    """Offsets beyond 32 bits in x, in the codes and in the result."""
+    rows, cols = 3, 200
+    pitch = (1 << 31) + 8
+    x = torch.empty(2 * pitch + 256, dtype=torch.bfloat16, device=DEV).as_strided((rows, cols), (pitch, 1))
+    x.copy_(torch.randn(rows, cols, generator=_gen(3), device=DEV))
+    q, s, qt, st = _quantize(x, "e4m3", False, True)
+    _check_codes(x.double().cpu().numpy(), "e4m3", False, q, s)
+    c = torch.empty(2 * pitch + 256, dtype=torch.bfloat16, device=DEV).as_strided((rows, rows), (pitch, 1))
+    _matmul((q, s), "e4m3", (q, s), "e4m3", cols, c)
+    v = torch.empty(rows, cols, device=DEV)
+    thc.thc_fp8_dequantize(q, s, thc.THC_E4M3, v)
+    want = v.double() @ v.double().t()
+    assert ((c.double() - want).abs() <= _sum_bound(v.double().abs() @ v.double().abs().t(), cols) + 2.0 ** -8 * want.abs()).all()
+
+
+def test_codes_beyond_4_gib():
+    """An operand of more than 2^32 bytes: its last rows."""
+    N, K, M = (1 << 20) + 3, 4224, 17
+    codes = torch.zeros(N * K, dtype=torch.uint8, device=DEV)
+    scales = torch.full((thc.thc_fp8_scale_bytes(N, K),), 127, dtype=torch.uint8, device=DEV)
+    a = _whole(M, K, "e4m3", 1)
+    b = _whole(40, K, "e4m3", 2)
+    codes[-40 * K:] = b[0]
+    bv = torch.tensor(O.code_values("e4m3")[b[0].cpu().numpy()].reshape(40, K), device=DEV)
+    c = torch.full((M, N), float("nan"), device=DEV)
+    _matmul(a, "e4m3", (codes, scales), "e4m3", K, c)
+    assert torch.equal(c[:, -40:].double(), a[2] @ bv.t()) and not c[:, :-40].any()
