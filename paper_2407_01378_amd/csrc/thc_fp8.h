@@ -10,6 +10,7 @@ namespace thc {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -93,6 +94,13 @@ __device__ __forceinline__ f32x4 bf16_mfma16(i32x8 a, i32x8 b, f32x4 d, uint32_t
         d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8_widen<FA>(a[2 * i], a[2 * i + 1], sa),
                                                     fp8_widen<FB>(b[2 * i], b[2 * i + 1], sb), d, 0, 0, 0);
     return d;
+}
+
+// The same over 64 values of k for 32 rows: lane l holds of row l % 32 the 32 codes of one half, l / 32.  Result: lane l
+// holds rows 8 (i / 4) + 4 (l / 32) + i % 4 of A, i < 16, column l % 32 of B.
+template <int FA, int FB>
+__device__ __forceinline__ f32x16 fp8_mfma32(i32x8 a, i32x8 b, f32x16 d, uint32_t scale_a, uint32_t scale_b) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, FA, FB, 0, (int)scale_a, 0, (int)scale_b);
 }
 
 }  // namespace thc
