@@ -18,7 +18,7 @@ __device__ __forceinline__ float load1(const void* p, bool bf16, uint64_t at) {
     return bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[at] << 16) : static_cast<const float*>(p)[at];
 }
 __device__ __forceinline__ void store1(void* p, bool bf16, uint64_t at, float v) {
-    if (bf16) static_cast<uint16_t*>(p)[at] = (uint16_t)bf16_rne(v);
+    if (bf16) static_cast<uint16_t*>(p)[at] = bf16_bits(v);
     else static_cast<float*>(p)[at] = v;
 }
 

@@ -11,53 +11,43 @@
 namespace thc {
 namespace {
 
-constexpr uint32_t kStep = 128;
+constexpr uint32_t kStep = 128, kHalf = 64;
 constexpr uint64_t kMaxGrid = 1ull << 23;   // workgroups of 256 threads: 2^31 threads
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-// 8 neighbouring values of a row of C.
+// 8 neighbouring values of a row of C, on the 16-byte grid.
 template <bool BF16>
-__device__ __forceinline__ void store8(const Fp8MatmulArgs& a, uint32_t m, uint32_t n, float (&v)[8], bool vector) {
-    const uint64_t at = (uint64_t)m * a.ldc + n;
-    if (vector && n + 8u <= a.N) {
-        if (BF16) {
-            uint4* c = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.c) + at);
-            if (a.accumulate) {
-                const uint4 old = *c;
-                const uint32_t o[4] = {old.x, old.y, old.z, old.w};
+struct Row8 {
+    uint4 w[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const void* c) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[2 * i] += __uint_as_float(o[i] << 16);
-                    v[2 * i + 1] += __uint_as_float(o[i] & 0xFFFF0000u);
-                }
-            }
-            uint32_t p[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = bf16_rne(v[2 * i]) | bf16_rne(v[2 * i + 1]) << 16;
-            *c = make_uint4(p[0], p[1], p[2], p[3]);
-        } else {
-            float4* c = reinterpret_cast<float4*>(static_cast<float*>(a.c) + at);
-            if (a.accumulate) {
-                const float4 x = c[0], y = c[1];
-                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-                v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-            }
-            c[0] = make_float4(v[0], v[1], v[2], v[3]);
-            c[1] = make_float4(v[4], v[5], v[6], v[7]);
-        }
-        return;
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = static_cast<const uint4*>(c)[i];
     }
+    __device__ __forceinline__ void add_to(float (&v)[8]) const {
+        const uint32_t x[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[BF16 ? 0 : 1].x, w[BF16 ? 0 : 1].y, w[BF16 ? 0 : 1].z, w[BF16 ? 0 : 1].w};
 #pragma unroll
-    for (uint32_t i = 0; i < 8u; ++i) {
-        if (n + i >= a.N) continue;
+        for (int i = 0; i < 8; ++i)
+            v[i] += BF16 ? (i & 1 ? bf16_high(x[i >> 1]) : bf16_low(x[i >> 1])) : __uint_as_float(x[i]);
+    }
+    static __device__ __forceinline__ void store(void* c, const float (&v)[8]) {
         if (BF16) {
-            uint16_t* c = static_cast<uint16_t*>(a.c) + at + i;
-            *c = (uint16_t)bf16_rne(a.accumulate ? v[i] + __uint_as_float((uint32_t)*c << 16) : v[i]);
+            *static_cast<uint4*>(c) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
         } else {
-            float* c = static_cast<float*>(a.c) + at + i;
-            *c = a.accumulate ? v[i] + *c : v[i];
+            static_cast<float4*>(c)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            static_cast<float4*>(c)[1] = make_float4(v[4], v[5], v[6], v[7]);
         }
+    }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void store1(void* c, float v, bool accumulate) {
+    if (BF16) {
+        uint16_t* p = static_cast<uint16_t*>(c);
+        *p = bf16_bits(accumulate ? v + bf16_low(*p) : v);
+    } else {
+        float* p = static_cast<float*>(c);
+        *p = accumulate ? v + *p : v;
     }
 }
 
@@ -75,59 +65,70 @@ __device__ __forceinline__ void place_tile(uint32_t id, uint32_t total, uint32_t
 template <int FA, int FB, bool EXACT, int MF, int NF>
 __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n, bool vector) {
     constexpr uint32_t BM = 64u * MF, BN = 64u * NF;
-    __shared__ __attribute__((aligned(1024))) uint8_t s0[(BM + BN) * kStep];
-    __shared__ __attribute__((aligned(1024))) uint8_t s1[(BM + BN) * kStep];
+    static_assert(MF == NF, "the four units of a step have one size");
+    // A step's codes are four units, the even and the odd halves of the waves' rows of A and of B; ten units fit LDS.  (Arrays of
+    // their own: that a fetch to one does not touch what is read from another has to be seen.)
+    constexpr uint32_t kUnitRows = 32u * MF, kUnit = kUnitRows * kStep, kSlots = 10;
+    __shared__ __attribute__((aligned(1024))) uint8_t s0[kUnit], s1[kUnit], s2[kUnit], s3[kUnit], s4[kUnit], s5[kUnit], s6[kUnit],
+        s7[kUnit], s8[kUnit], s9[kUnit];
+    uint8_t* const slots[kSlots] = {s0, s1, s2, s3, s4, s5, s6, s7, s8, s9};
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const uint32_t x = lane & 31u, h = lane >> 5, wm = wave & 1u, wn = wave >> 1;
     uint32_t tm, tn;
     place_tile(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
     const uint32_t m0 = tm * BM, n0 = tn * BN, steps = (a.K + kStep - 1u) / kStep, ld = steps * kStep;
 
-    // memory -> LDS: a wave moves 8 rows at a time, lane l the piece that belongs at place l % 8 of row l / 8
+    // memory -> LDS: a wave moves 8 rows (whole lines of memory) at a time, lane l the piece of 16 codes that belongs at place
+    // l % 8 of row l / 8.  Piece c of a row lies at place c ^ key: two rows fill all banks, and of 16 lanes that read
+    // one piece of their rows at a time no two may share a place in rows of the same parity.  key = bits 1, 2, 3 of the
+    // row, in the order in which lanes take the rows.
     const uint32_t left_m = a.M - m0, left_n = a.N - n0;
     const uint32_t rows_m = left_m < BM ? left_m : BM, rows_n = left_n < BN ? left_n : BN;
     const auto src_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.a + (uint64_t)m0 * ld), 0, rows_m * ld, 0x00020000);
     const auto src_b = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.b + (uint64_t)n0 * ld), 0, rows_n * ld, 0x00020000);
-    uint32_t off_a[BM / 32u], off_b[BN / 32u];
-    const uint32_t key_b = ((lane >> 3) & 3u) | (wave & 1u) << 2;
+    uint32_t off[4][MF];
+    const uint32_t key_a = lane >> 4 | (wave & 1u) << 2, key_b = ((lane >> 4) & 1u) | (wave & 1u) << 1 | (lane >> 5) << 2;
 #pragma unroll
-    for (uint32_t i = 0; i < BM / 32u; ++i) {
-        const uint32_t r = 8u * (wave + 4u * i) + (lane >> 3);
-        off_a[i] = (r < rows_m ? r : rows_m - 1u) * ld + (((lane & 7u) ^ (lane >> 3)) << 4);
-    }
+    for (uint32_t i = 0; i < MF; ++i) {
+        const uint32_t q = 8u * (wave + 4u * i) + (lane >> 3);   // row of the unit
+        const uint32_t r = q / (16u * MF) * (32u * MF) + q % (16u * MF);
 #pragma unroll
-    for (uint32_t i = 0; i < BN / 32u; ++i) {
-        const uint32_t r = 8u * (wave + 4u * i) + (lane >> 3);
-        off_b[i] = (r < rows_n ? r : rows_n - 1u) * ld + (((lane & 7u) ^ key_b) << 4);
+        for (uint32_t u = 0; u < 2u; ++u) {
+            const uint32_t ru = r + u * 16u * MF;
+            off[u][i] = (ru < rows_m ? ru : rows_m - 1u) * ld + (((lane & 7u) ^ key_a) << 4);
+            off[2u + u][i] = (ru < rows_n ? ru : rows_n - 1u) * ld + (((lane & 7u) ^ key_b) << 4);
+        }
     }
     uint32_t base = wave * 1024u;
-    auto fetch = [&](uint8_t* s, uint32_t k) {
-        asm volatile("" : "+s"(base));   // (32 places in LDS, kept across the loop, would not fit the scalar registers)
+    auto fetch = [&](uint8_t* s, auto unit, uint32_t step) {
+        constexpr uint32_t u = decltype(unit)::value;
+        asm volatile("" : "+s"(base));   // (all places in LDS, kept across the loop, would not fit the scalar registers)
+        const int k = (int)(step < steps ? step * kStep : 0u);   // (behind the last step: not used)
 #pragma unroll
-        for (uint32_t i = 0; i < BM / 32u; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(src_a, (lds_void*)(s + base + i * 4096u), 16, (int)off_a[i], (int)k, 0, 0);
-#pragma unroll
-        for (uint32_t i = 0; i < BN / 32u; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(src_b, (lds_void*)(s + base + BM * kStep + i * 4096u), 16, (int)off_b[i], (int)k, 0, 0);
+        for (uint32_t i = 0; i < MF; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(u < 2u ? src_a : src_b, (lds_void*)(s + base + i * 4096u), 16, (int)off[u][i], k, 0, 0);
     };
 
     // LDS -> registers.  Rows of B are taken in the order with bits 2 and 3 exchanged, which gives a lane 8
     // neighbouring columns of C.
     const uint32_t xb = (x & 0x13u) | (x & 4u) << 1 | (x & 8u) >> 1;
-    const uint32_t at_a = (wm * 32u * MF + x) * kStep + (((2u * h) ^ (x & 7u)) << 4);
-    const uint32_t at_b = (BM + wn * 32u * NF + xb) * kStep + (((2u * h) ^ (x & 7u)) << 4);
-    auto read = [&](const uint8_t* s, uint32_t half, i32x8 (&fa)[MF], i32x8 (&fb)[NF]) {
-        auto piece = [&](uint32_t at) {
+    const uint32_t at_a = (wm * 16u * MF + x) * kStep + (((2u * h) ^ ((x >> 1) & 7u)) << 4);
+    const uint32_t at_b = (wn * 16u * MF + xb) * kStep + (((2u * h) ^ ((x >> 1) & 7u)) << 4);
+    auto read = [&](auto first, uint32_t half, i32x8 (&fa)[MF], i32x8 (&fb)[NF]) {   // first: the step's first unit
+        constexpr uint32_t u = decltype(first)::value;
+        auto piece = [&](const uint8_t* s, uint32_t at) {
             const uint4 lo = *reinterpret_cast<const uint4*>(s + at), hi = *reinterpret_cast<const uint4*>(s + (at ^ 16u));
             return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         };
 #pragma unroll
-        for (uint32_t f = 0; f < MF; ++f) fa[f] = piece((at_a ^ (half << 6)) + f * 32u * kStep);
+        for (uint32_t f = 0; f < MF; ++f)
+            fa[f] = piece(slots[(u + f / (MF / 2u)) % kSlots], (at_a ^ (half << 6)) + f % (MF / 2u) * 32u * kStep);
 #pragma unroll
-        for (uint32_t f = 0; f < NF; ++f) fb[f] = piece((at_b ^ (half << 6)) + f * 32u * kStep);
+        for (uint32_t f = 0; f < NF; ++f)
+            fb[f] = piece(slots[(u + 2u + f / (NF / 2u)) % kSlots], (at_b ^ (half << 6)) + f % (NF / 2u) * 32u * kStep);
     };
 
-    // a block's scale bytes
+    // scale words: four blocks each
     uint32_t row_a[MF], row_b[NF];   // in bytes from the tile's first row
 #pragma unroll
     for (uint32_t f = 0; f < MF; ++f) {
@@ -139,15 +140,17 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         const uint32_t r = wn * 32u * NF + f * 32u + xb;
         row_b[f] = 4u * (r < rows_n ? r : rows_n - 1u);
     }
-    auto scales = [&](uint32_t j, uint32_t (&wa)[MF], uint32_t (&wb)[NF]) {
-        const uint8_t* pa = reinterpret_cast<const uint8_t*>(a.a_scales + (uint64_t)(j >> 2) * a.M + m0) + (j & 3u);
-        const uint8_t* pb = reinterpret_cast<const uint8_t*>(a.b_scales + (uint64_t)(j >> 2) * a.N + n0) + (j & 3u);
+    auto scales = [&](uint32_t word, uint32_t (&wa)[MF], uint32_t (&wb)[NF]) {
+        const uint8_t* pa = reinterpret_cast<const uint8_t*>(a.a_scales + (uint64_t)word * a.M + m0);
+        const uint8_t* pb = reinterpret_cast<const uint8_t*>(a.b_scales + (uint64_t)word * a.N + n0);
 #pragma unroll
-        for (uint32_t f = 0; f < MF; ++f) wa[f] = pa[row_a[f]];
+        for (uint32_t f = 0; f < MF; ++f) wa[f] = *reinterpret_cast<const uint32_t*>(pa + row_a[f]);
 #pragma unroll
-        for (uint32_t f = 0; f < NF; ++f) wb[f] = pb[row_b[f]];
+        for (uint32_t f = 0; f < NF; ++f) wb[f] = *reinterpret_cast<const uint32_t*>(pb + row_b[f]);
     };
 
+    const uint32_t words = (steps + 3u) / 4u;
+    uint32_t sa[MF], sb[NF], next_a[MF], next_b[NF];
     f32x16 acc[MF][NF];
 #pragma unroll
     for (int i = 0; i < MF; ++i)
@@ -155,7 +158,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         for (int j = 0; j < NF; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    auto multiply = [&](const i32x8 (&fa)[MF], const i32x8 (&fb)[NF], const uint32_t (&sa)[MF], const uint32_t (&sb)[NF]) {
+    auto multiply = [&](const i32x8 (&fa)[MF], const i32x8 (&fb)[NF]) {
         if constexpr (EXACT) {
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
@@ -193,81 +196,157 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    // The order of a half: reads from LDS among its first products, fetches among the others.
-    auto alternate = [&](bool fetches) {
-#pragma unroll
-        for (int i = 0; i < MF + NF; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, EXACT ? 4 : 1, 0);              // matrix instruction
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);                          // LDS read
-            if (!fetches) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);            // load
-        }
-#pragma unroll
-        for (int i = 0; i < MF + NF; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, EXACT ? 4 : 1, 0);
-            if (fetches) __builtin_amdgcn_sched_group_barrier(0x010, 2, 0);
-        }
-    };
-
+    // A step's first half (64 k) is multiplied while its second one is read, and its second half while the next
+    // step's first one is.  Behind the first half every wave has read all of the step's units and has waited for what
+    // it fetched of the next step, with the 2 units fetched last still on their way: from there on two units of the step
+    // after the next one, and in the next first half two of the one behind it, go where the step's were.
     i32x8 fa0[MF], fb0[NF], fa1[MF], fb1[NF];
-    uint32_t sa0[MF], sb0[NF], sa1[MF], sb1[NF];
-    const uint32_t last = steps - 1u;
-    fetch(s0, 0);
-    scales(0, sa0, sb0);
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    fetch(s1, last < 1u ? 0u : kStep);
-    read(s0, 0, fa0, fb0);
-
-    // One step: its second half is read while the first one is multiplied, the next step's first half (which has
-    // arrived when every wave has waited for its part) while the second one is.  Behind the last step the last codes
-    // are fetched again, and not used.
-    auto step = [&](uint8_t* cur, uint8_t* nxt, uint32_t k, const uint32_t (&sa)[MF], const uint32_t (&sb)[NF],
-                    uint32_t (&next_a)[MF], uint32_t (&next_b)[NF]) {
-        from_here(fa0, fb0);
-        read(cur, 1, fa1, fb1);
-        scales(k + 1u < steps ? k + 1u : last, next_a, next_b);
-        multiply(fa0, fb0, sa, sb);
-        alternate(false);
+    auto order = [&]() {   // reads from LDS among the first products, then fetches
+#pragma unroll
+        for (int i = 0; i < (MF + NF) / 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, EXACT ? MF : 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * MF; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, EXACT ? MF : 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+        }
         up_to_here();
-        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+    };
+    auto step = [&](auto phase, uint32_t k) {   // phase: k mod 5
+        constexpr uint32_t u = 4u * decltype(phase)::value;
+        from_here(fa0, fb0);
+        read(std::integral_constant<uint32_t, u>{}, 1, fa1, fb1);
+        fetch(slots[(u + 8u) % kSlots], std::integral_constant<uint32_t, 0>{}, k + 2u);
+        fetch(slots[(u + 9u) % kSlots], std::integral_constant<uint32_t, 1>{}, k + 2u);
+        multiply(fa0, fb0);
+        order();
+        constexpr uint32_t kLeft = 2u * MF;
+        __builtin_amdgcn_s_waitcnt((kLeft & 15u) | (kLeft >> 4) << 14 | 7u << 4);   // vmcnt(kLeft) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         from_here(fa1, fb1);
-        read(nxt, 0, fa0, fb0);
-        fetch(cur, (k + 2u < steps ? k + 2u : last) * kStep);
-        multiply(fa1, fb1, sa, sb);
-        alternate(true);
-        up_to_here();
+        read(std::integral_constant<uint32_t, u + 4u>{}, 0, fa0, fb0);
+        fetch(slots[(u + 10u) % kSlots], std::integral_constant<uint32_t, 2>{}, k + 2u);
+        fetch(slots[(u + 11u) % kSlots], std::integral_constant<uint32_t, 3>{}, k + 2u);
+        multiply(fa1, fb1);
+        order();
+        if ((k & 3u) == 3u) {   // (moved, not renamed: a load that may be on its way would be waited for in every step)
+#pragma unroll
+            for (int i = 0; i < MF; ++i) asm volatile("v_mov_b32 %0, %1" : "=v"(sa[i]) : "v"(next_a[i]));
+#pragma unroll
+            for (int j = 0; j < NF; ++j) asm volatile("v_mov_b32 %0, %1" : "=v"(sb[j]) : "v"(next_b[j]));
+            const uint32_t w = (k >> 2) + 2u;
+            scales(w < words ? w : 0u, next_a, next_b);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MF; ++i) sa[i] >>= 8;
+#pragma unroll
+            for (int j = 0; j < NF; ++j) sb[j] >>= 8;
+        }
     };
-    uint32_t k = 0;
-    for (; k + 1u < steps; k += 2u) {
-        step(s0, s1, k, sa0, sb0, sa1, sb1);
-        step(s1, s0, k + 1u, sa1, sb1, sa0, sb0);
-    }
-    if (k < steps) step(s0, s1, k, sa0, sb0, sa1, sb1);
-
-    // C by way of LDS, 32 rows of a wave at a time, so that a row of it is stored by neighbouring lanes.
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // (the last fetch)
+    scales(0, sa, sb);
+    scales(words > 1u ? 1u : 0u, next_a, next_b);
+    fetch(s0, std::integral_constant<uint32_t, 0>{}, 0);
+    fetch(s1, std::integral_constant<uint32_t, 1>{}, 0);
+    fetch(s2, std::integral_constant<uint32_t, 2>{}, 0);
+    fetch(s3, std::integral_constant<uint32_t, 3>{}, 0);
+    fetch(s4, std::integral_constant<uint32_t, 0>{}, 1);
+    fetch(s5, std::integral_constant<uint32_t, 1>{}, 1);
+    fetch(s6, std::integral_constant<uint32_t, 2>{}, 1);
+    fetch(s7, std::integral_constant<uint32_t, 3>{}, 1);
+    constexpr uint32_t kNext = 4u * MF;
+    __builtin_amdgcn_s_waitcnt((kNext & 15u) | (kNext >> 4) << 14 | 0xF70u);   // vmcnt(kNext): step 0
     __builtin_amdgcn_s_barrier();
-    constexpr uint32_t kPitch = 32u * NF + 4u;
-    float* strip = reinterpret_cast<float*>(wave < 2u ? s0 : s1) + (wave & 1u) * 32u * kPitch;
+    __builtin_amdgcn_sched_barrier(0);
+    read(std::integral_constant<uint32_t, 0>{}, 0, fa0, fb0);
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t k = 0;
+    for (; k + 4u < steps; k += 5u) {
+        step(std::integral_constant<uint32_t, 0>{}, k);
+        step(std::integral_constant<uint32_t, 1>{}, k + 1u);
+        step(std::integral_constant<uint32_t, 2>{}, k + 2u);
+        step(std::integral_constant<uint32_t, 3>{}, k + 3u);
+        step(std::integral_constant<uint32_t, 4>{}, k + 4u);
+    }
+    if (k < steps) step(std::integral_constant<uint32_t, 0>{}, k);
+    if (k + 1u < steps) step(std::integral_constant<uint32_t, 1>{}, k + 1u);
+    if (k + 2u < steps) step(std::integral_constant<uint32_t, 2>{}, k + 2u);
+    if (k + 3u < steps) step(std::integral_constant<uint32_t, 3>{}, k + 3u);
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // (what was fetched behind the last step)
+
+    constexpr bool BF16 = !EXACT;
+    constexpr uint32_t kSize = BF16 ? 2u : 4u, kCols = 32u * NF;
+    const uint32_t mw = m0 + wm * 32u * MF, nw = n0 + wn * kCols;
+    uint8_t* c = static_cast<uint8_t*>(a.c);
+    if (vector && n0 + BN <= a.N) {
+        // A whole tile with rows on the 16-byte grid: straight from the registers.
+        auto rows = [&](auto add) {
+#pragma unroll
+            for (uint32_t i = 0; i < MF; ++i) {
+                const uint32_t m = mw + i * 32u + x;
+                if (m >= a.M) continue;
+                uint8_t* at = c + ((uint64_t)m * a.ldc + nw + 8u * h) * kSize;
+                Row8<BF16> old[NF][2];
+                if (decltype(add)::value) {
+#pragma unroll
+                    for (uint32_t j = 0; j < 2u * NF; ++j) old[j >> 1][j & 1u].load(at + j * 16u * kSize);
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < 2u * NF; ++j) {
+                    float v[8];
+#pragma unroll
+                    for (uint32_t e = 0; e < 8u; ++e) v[e] = acc[i][j >> 1][8u * (j & 1u) + e];
+                    if (decltype(add)::value) old[j >> 1][j & 1u].add_to(v);
+                    Row8<BF16>::store(at + j * 16u * kSize, v);
+                }
+            }
+        };
+        if (a.accumulate) rows(std::true_type{});
+        else rows(std::false_type{});
+        return;
+    }
+    // Otherwise by way of LDS, 32 rows of a wave at a time, so that neighbouring lanes store neighbouring values.
+    __builtin_amdgcn_s_barrier();
+    if (nw >= a.N) return;
+    // (two units to a strip, one behind the other)
+    constexpr uint32_t kPitch = kCols + 4u, kHalfRows = 16u;
+    static_assert(kHalfRows * kPitch * sizeof(float) <= kUnit, "half a strip fits a unit");
+    float* const lower = reinterpret_cast<float*>(wave == 0u ? s0 : wave == 1u ? s1 : wave == 2u ? s2 : s3);
+    float* const upper = reinterpret_cast<float*>(wave == 0u ? s4 : wave == 1u ? s5 : wave == 2u ? s6 : s7);
+    auto strip = [&](uint32_t r) { return (r < kHalfRows ? lower : upper) + (r % kHalfRows) * kPitch; };
+    const uint32_t cols = a.N - nw < kCols ? a.N - nw : kCols;
 #pragma unroll
     for (uint32_t i = 0; i < MF; ++i) {
 #pragma unroll
         for (uint32_t j = 0; j < NF; ++j)
 #pragma unroll
             for (uint32_t q = 0; q < 4u; ++q) {
-                float* at = strip + x * kPitch + j * 32u + 16u * (q >> 1) + 8u * h + 4u * (q & 1u);
+                float* at = strip(x) + j * 32u + 16u * (q >> 1) + 8u * h + 4u * (q & 1u);
                 *reinterpret_cast<float4*>(at) = make_float4(acc[i][j][4u * q], acc[i][j][4u * q + 1u], acc[i][j][4u * q + 2u], acc[i][j][4u * q + 3u]);
             }
-        constexpr uint32_t kLanes = 4u * NF, kRows = 64u / kLanes;   // lanes of a row, rows at a time
-#pragma unroll 1
-        for (uint32_t r = lane / kLanes; r < 32u; r += kRows) {
-            const uint32_t c = lane % kLanes * 8u, m = m0 + wm * 32u * MF + i * 32u + r, n = n0 + wn * 32u * NF + c;
-            const float4 lo = *reinterpret_cast<const float4*>(strip + r * kPitch + c);
-            const float4 hi = *reinterpret_cast<const float4*>(strip + r * kPitch + c + 4u);
-            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            if (m < a.M && n < a.N) store8<!EXACT>(a, m, n, v, vector);
+        const uint32_t m1 = mw + i * 32u, rows = m1 >= a.M ? 0u : a.M - m1 < 32u ? a.M - m1 : 32u;
+        if (BF16 && !a.accumulate) {
+            // pairs on the 4-byte grid, then the values left over at a row's ends
+#pragma unroll 4
+            for (uint32_t r = 0; r < rows; ++r) {
+                uint8_t* at = c + ((uint64_t)(m1 + r) * a.ldc + nw) * 2u;
+                const uint32_t n = 2u * lane + (uint32_t)(reinterpret_cast<uintptr_t>(at) >> 1 & 1u);
+                if (n + 1u < cols) *reinterpret_cast<uint32_t*>(at + 2u * n) = bf16_pair(strip(r)[n], strip(r)[n + 1u]);
+            }
+            const uint32_t r = lane >> 1;
+            if (r < rows) {
+                uint8_t* at = c + ((uint64_t)(m1 + r) * a.ldc + nw) * 2u;
+                const uint32_t odd = (uint32_t)(reinterpret_cast<uintptr_t>(at) >> 1 & 1u), n = lane & 1u ? cols - 1u : 0u;
+                if (lane & 1u ? ((cols - odd) & 1u) != 0u && n >= odd : odd != 0u) store1<true>(at + 2u * n, strip(r)[n], false);
+            }
+        } else {
+#pragma unroll 2
+            for (uint32_t r = 0; r < rows; ++r)
+#pragma unroll
+                for (uint32_t n = lane; n < kCols; n += 64u)
+                    if (n < cols) store1<BF16>(c + ((uint64_t)(m1 + r) * a.ldc + nw + n) * kSize, strip(r)[n], a.accumulate);
         }
     }
 }

@@ -202,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void fp8_dequantize_kernel(const uint8_t*
                 for (int k = 0; k < 2; ++k) {
                     uint32_t p[4];
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) p[d] = bf16_rne(v[8 * k + 2 * d]) | bf16_rne(v[8 * k + 2 * d + 1]) << 16;
+                    for (int d = 0; d < 4; ++d) p[d] = bf16_pair(v[8 * k + 2 * d], v[8 * k + 2 * d + 1]);
                     o[k] = make_uint4(p[0], p[1], p[2], p[3]);
                 }
             } else {
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void fp8_dequantize_kernel(const uint8_t*
         for (uint32_t k = 0; k < 16u; ++k) {
             if (c + k >= cols) continue;
             const uint64_t at = (uint64_t)r * ld + c + k;
-            if (BF16OUT) static_cast<uint16_t*>(out)[at] = (uint16_t)bf16_rne(v[k]);
+            if (BF16OUT) static_cast<uint16_t*>(out)[at] = bf16_bits(v[k]);
             else static_cast<float*>(out)[at] = v[k];
         }
     }
