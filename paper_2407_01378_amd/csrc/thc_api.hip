@@ -1211,9 +1211,12 @@ int thc_fp8_matmul(const uint8_t* a, const uint8_t* a_scales, int a_format, cons
     return finish(thc::launch_fp8_matmul(m, static_cast<hipStream_t>(stream)));
 }
 
+// Few rows are quantized by the workgroups of the product themselves.
+static bool linear_in_one_launch(uint64_t M, uint64_t, uint64_t K) { return M <= thc::kFp8NarrowRows && K != 0; }
+
 // The workspace of thc_fp8_linear: the codes of x, its scales, the product's own workspace.
 uint64_t thc_fp8_linear_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
-    if (!fp8_product_in_range(M, N, K) || M == 0 || N == 0) return 0;
+    if (!fp8_product_in_range(M, N, K) || M == 0 || N == 0 || linear_in_one_launch(M, N, K)) return 0;
     return M * thc::fp8_row_bytes(K) + round16(4 * thc::fp8_scale_words(M, K)) + thc::fp8_matmul_workspace_bytes(M, N, K);
 }
 
@@ -1233,6 +1236,23 @@ int thc_fp8_linear(const void* x, thc_dtype dt, uint64_t M, uint64_t K, uint64_t
     if (!aligned(x, dtype_bytes(dt)) || !aligned(b, 16) || !aligned(b_scales, 16) || !aligned(out, dtype_bytes(out_dt)) ||
         (need != 0 && !aligned(workspace, 16)))
         return THC_ERR_ALIGN;
+    if (linear_in_one_launch(M, N, K)) {
+        thc::Fp8NarrowArgs a{};
+        a.x = x;
+        a.ldx = ldx;
+        a.source = dt == THC_BF16 ? 1 : 2;
+        a.b = b;
+        a.b_scales = reinterpret_cast<const uint32_t*>(b_scales);
+        a.M = (uint32_t)M;
+        a.N = (uint32_t)N;
+        a.K = (uint32_t)K;
+        a.a_e5m2 = x_format == THC_E5M2;
+        a.b_e5m2 = b_format == THC_E5M2;
+        a.out_bf16 = out_dt == THC_BF16;
+        a.c = out;
+        a.ldc = ldo;
+        return finish(thc::launch_fp8_narrow(a, static_cast<hipStream_t>(stream)));
+    }
     uint8_t* codes = static_cast<uint8_t*>(workspace);
     uint8_t* scales = codes + M * thc::fp8_row_bytes(K);
     const uint64_t used = M * thc::fp8_row_bytes(K) + round16(4 * thc::fp8_scale_words(M, K));

@@ -25,22 +25,42 @@ __device__ __forceinline__ uint32_t fp8_scale_byte(uint32_t amax_bits) {
     return amax_bits >= 0x7F800000u ? 255u : (uint32_t)e;
 }
 
-// 2^(127 - e) for e <= 247, which covers every finite block; a product with it is exact, or below
-// the format's smallest value by far.
-__device__ __forceinline__ float fp8_inverse_scale(uint32_t e) { return __uint_as_float((254u - (e < 254u ? e : 253u)) << 23); }
+// The fp32 number whose exponent field is a scale word's low byte: 2^(e - 127).
+__device__ __forceinline__ float fp8_scale(uint32_t word) { return __uint_as_float((word & 0xFFu) << 23); }
 
-// Codes of four values (to nearest, ties to even), lowest byte first.
+// Codes of four values divided by the scale 2^(e - 127), given as the fp32 number with exponent field e (to nearest, ties
+// to even), lowest byte first.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
 template <bool E5M2>
-__device__ __forceinline__ uint32_t fp8_codes(float a, float b, float c, float d) {
-    int w = 0;
+__device__ __forceinline__ uint32_t fp8_codes(float a, float b, float c, float d, float scale) {
+    i16x2 w = {0, 0};
     if (E5M2) {
-        w = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, w, false);
-        w = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, w, true);
+        w = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(w, a, b, scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(w, c, d, scale, true);
     } else {
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true);
     }
-    return (uint32_t)w;
+    return __builtin_bit_cast(uint32_t, w);
+}
+// The same for four bf16 values in two words.
+template <bool E5M2>
+__device__ __forceinline__ uint32_t fp8_codes_bf16(uint32_t ab, uint32_t cd, float scale) {
+    const bf16x2 lo = __builtin_bit_cast(bf16x2, ab), hi = __builtin_bit_cast(bf16x2, cd);
+    i16x2 w = {0, 0};
+    if (E5M2) {
+        w = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(w, lo, scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(w, hi, scale, true);
+    } else {
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, lo, scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, hi, scale, true);
+    }
+    return __builtin_bit_cast(uint32_t, w);
+}
+// Larger of two pairs of 16-bit numbers (magnitudes of bf16 values order as whole numbers).
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
 
 // Two values as bf16 (to nearest, ties to even), the first one in the low half.
@@ -89,8 +109,6 @@ __device__ __forceinline__ bf16x8 fp8_widen(int lo, int hi, float scale) {
     return bf16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
 }
 
-__device__ __forceinline__ float fp8_scale(uint32_t word) { return __uint_as_float((word & 0xFFu) << 23); }
-
 template <int FA, int FB>
 __device__ __forceinline__ f32x4 bf16_mfma16(i32x8 a, i32x8 b, f32x4 d, uint32_t scale_a, uint32_t scale_b) {
     const float sa = fp8_scale(scale_a), sb = fp8_scale(scale_b);
@@ -106,6 +124,41 @@ __device__ __forceinline__ f32x4 bf16_mfma16(i32x8 a, i32x8 b, f32x4 d, uint32_t
 template <int FA, int FB>
 __device__ __forceinline__ f32x16 fp8_mfma32(i32x8 a, i32x8 b, f32x16 d, uint32_t scale_a, uint32_t scale_b) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, FA, FB, 0, (int)scale_a, 0, (int)scale_b);
+}
+
+// 8 neighbouring values of a row of C, on the 16-byte grid.
+template <bool BF16>
+struct Row8 {
+    uint4 w[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const void* c) {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = static_cast<const uint4*>(c)[i];
+    }
+    __device__ __forceinline__ void add_to(float (&v)[8]) const {
+        const uint32_t x[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[BF16 ? 0 : 1].x, w[BF16 ? 0 : 1].y, w[BF16 ? 0 : 1].z, w[BF16 ? 0 : 1].w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] += BF16 ? (i & 1 ? bf16_high(x[i >> 1]) : bf16_low(x[i >> 1])) : __uint_as_float(x[i]);
+    }
+    static __device__ __forceinline__ void store(void* c, const float (&v)[8]) {
+        if (BF16) {
+            *static_cast<uint4*>(c) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+        } else {
+            static_cast<float4*>(c)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            static_cast<float4*>(c)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+    }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void store1(void* c, float v, bool accumulate) {
+    if (BF16) {
+        uint16_t* p = static_cast<uint16_t*>(c);
+        *p = bf16_bits(accumulate ? v + bf16_low(*p) : v);
+    } else {
+        float* p = static_cast<float*>(c);
+        *p = accumulate ? v + *p : v;
+    }
 }
 
 }  // namespace thc

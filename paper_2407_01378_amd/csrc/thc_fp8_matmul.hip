@@ -16,41 +16,6 @@ constexpr uint64_t kMaxGrid = 1ull << 23;   // workgroups of 256 threads: 2^31 t
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-// 8 neighbouring values of a row of C, on the 16-byte grid.
-template <bool BF16>
-struct Row8 {
-    uint4 w[BF16 ? 1 : 2];
-    __device__ __forceinline__ void load(const void* c) {
-#pragma unroll
-        for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = static_cast<const uint4*>(c)[i];
-    }
-    __device__ __forceinline__ void add_to(float (&v)[8]) const {
-        const uint32_t x[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[BF16 ? 0 : 1].x, w[BF16 ? 0 : 1].y, w[BF16 ? 0 : 1].z, w[BF16 ? 0 : 1].w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] += BF16 ? (i & 1 ? bf16_high(x[i >> 1]) : bf16_low(x[i >> 1])) : __uint_as_float(x[i]);
-    }
-    static __device__ __forceinline__ void store(void* c, const float (&v)[8]) {
-        if (BF16) {
-            *static_cast<uint4*>(c) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
-        } else {
-            static_cast<float4*>(c)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            static_cast<float4*>(c)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        }
-    }
-};
-
-template <bool BF16>
-__device__ __forceinline__ void store1(void* c, float v, bool accumulate) {
-    if (BF16) {
-        uint16_t* p = static_cast<uint16_t*>(c);
-        *p = bf16_bits(accumulate ? v + bf16_low(*p) : v);
-    } else {
-        float* p = static_cast<float*>(c);
-        *p = accumulate ? v + *p : v;
-    }
-}
-
 // The place of workgroup `id` among `total` tiles: workgroups go round the 8 dies in turn, and each die's workgroups take a
 // contiguous run of tiles, in columns of 4 tiles in m, so that what a die reads at a time is few rows of A and B.
 __device__ __forceinline__ void place_tile(uint32_t id, uint32_t total, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
@@ -371,6 +336,11 @@ hipError_t launch_fp8_matmul(const Fp8MatmulArgs& a, hipStream_t stream) {
         const uint64_t blocks = ((uint64_t)a.M * a.N + 255u) / 256u;
         zero_matrix_kernel<<<(uint32_t)(blocks < 4096u ? blocks : 4096u), 256, 0, stream>>>(a);
         return hipGetLastError();
+    }
+    if (a.M <= kFp8NarrowRows) {
+        Fp8NarrowArgs narrow{};
+        static_cast<Fp8MatmulArgs&>(narrow) = a;
+        return launch_fp8_narrow(narrow, stream);
     }
     const uint32_t size = a.out_bf16 ? 2u : 4u;
     const bool vector = (reinterpret_cast<uintptr_t>(a.c) & 15u) == 0 && a.ldc * size % 16u == 0;

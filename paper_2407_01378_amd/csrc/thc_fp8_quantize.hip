@@ -139,10 +139,10 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs 
             for (uint32_t p = 0; p < 8u; ++p) {
                 if (r0 + p >= a.rows) continue;
                 const uint32_t e = fp8_scale_byte<E5M2>(rm[p]);
-                const float m = fp8_inverse_scale(e);
+                const float scale = fp8_scale(e);
                 uint2 w;
-                w.x = fp8_codes<E5M2>(v[p][0] * m, v[p][1] * m, v[p][2] * m, v[p][3] * m);
-                w.y = fp8_codes<E5M2>(v[p][4] * m, v[p][5] * m, v[p][6] * m, v[p][7] * m);
+                w.x = fp8_codes<E5M2>(v[p][0], v[p][1], v[p][2], v[p][3], scale);
+                w.y = fp8_codes<E5M2>(v[p][4], v[p][5], v[p][6], v[p][7], scale);
                 if (e == 255u) w.x = w.y = 0x7F7F7F7Fu;
                 *reinterpret_cast<uint2*>(a.q + (uint64_t)(r0 + p) * q_ld + c0) = w;
             }
@@ -152,10 +152,10 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs 
 #pragma unroll
             for (uint32_t j = 0; j < 8u; ++j) {
                 const uint32_t e = s_col[cg * 8u + j];
-                const float m = fp8_inverse_scale(e);
+                const float scale = fp8_scale(e);
                 uint2 w;
-                w.x = fp8_codes<E5M2>(v[0][j] * m, v[1][j] * m, v[2][j] * m, v[3][j] * m);
-                w.y = fp8_codes<E5M2>(v[4][j] * m, v[5][j] * m, v[6][j] * m, v[7][j] * m);
+                w.x = fp8_codes<E5M2>(v[0][j], v[1][j], v[2][j], v[3][j], scale);
+                w.y = fp8_codes<E5M2>(v[4][j], v[5][j], v[6][j], v[7][j], scale);
                 if (e == 255u) w.x = w.y = 0x7F7F7F7Fu;
                 s_code[cg * 8u + j][rg ^ cg] = w;   // (columns 8 apart fall into the same banks)
             }

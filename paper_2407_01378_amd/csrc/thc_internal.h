@@ -257,6 +257,14 @@ struct Fp8MatmulArgs {
 };
 uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
 hipError_t launch_fp8_matmul(const Fp8MatmulArgs& a, hipStream_t stream);
+// Few rows of A, given as codes (source 0) or as values to be quantized on the way (1 = bf16, 2 = fp32); K > 0.
+constexpr uint32_t kFp8NarrowRows = 32;
+struct Fp8NarrowArgs : Fp8MatmulArgs {
+    const void* x;
+    uint64_t ldx;
+    uint32_t source;
+};
+hipError_t launch_fp8_narrow(const Fp8NarrowArgs& a, hipStream_t stream);
 
 // ---- embedding (thc_embed.hip) -----------------------------------------------------------------
 struct EmbedArgs {

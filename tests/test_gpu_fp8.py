@@ -377,3 +377,23 @@ def test_codes_beyond_4_gib():
     c = torch.full((M, N), float("nan"), device=DEV)
     _matmul(a, "e4m3", (codes, scales), "e4m3", K, c)
     assert torch.equal(c[:, -40:].double(), a[2] @ bv.t()) and not c[:, :-40].any()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_blocks_at_the_lower_end(fmt, dt):
+    """Blocks whose scale is 2^-127 or just above: subnormal values among them."""
+    g = _gen(6)
+    x = torch.randn(20, 640, generator=g, device=DEV)
+    x *= 2.0 ** torch.randint(-148, -108, (20, 5), generator=g, device=DEV).double().repeat_interleave(128, 1)
+    x = x.float().to(DT[dt])
+    x64 = x.double().cpu().numpy()
+    assert (O.quantize(x64, fmt)[1] == 0).any() and (O.quantize(x64, fmt)[1] > 0).any()
+    q, s, qt, st = _quantize(x, fmt, False, True)
+    _check_codes(x64, fmt, False, q, s)
+    _check_codes(np.ascontiguousarray(x64.T), fmt, False, qt, st)
+    w = _whole(30, 640, "e4m3", 4)
+    y, z = torch.empty(20, 30, device=DEV), torch.empty(20, 30, device=DEV)
+    thc.thc_fp8_linear(x, CODE[fmt], w[0], w[1], thc.THC_E4M3, y, _ws(thc.thc_fp8_linear_workspace_bytes(20, 30, 640)))
+    _matmul((q, s), fmt, w, "e4m3", 640, z)
+    assert torch.equal(y, z)
