@@ -1170,8 +1170,9 @@ int thc_fp8_dequantize(const uint8_t* q, const uint8_t* scales, int format, uint
                                              static_cast<hipStream_t>(stream)));
 }
 
+static constexpr uint64_t kMaxProductRows = 1ull << 26;    // of A and of B: 2^22 workgroups for a single row of the other
 static bool fp8_product_in_range(uint64_t M, uint64_t N, uint64_t K) {
-    return M <= kMaxRows && N <= kMaxRows && K <= kMaxContracted;
+    return M <= kMaxProductRows && N <= kMaxProductRows && K <= kMaxContracted;
 }
 
 uint64_t thc_fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
@@ -1212,11 +1213,12 @@ int thc_fp8_matmul(const uint8_t* a, const uint8_t* a_scales, int a_format, cons
 }
 
 // Few rows are quantized by the workgroups of the product themselves.
-static bool linear_in_one_launch(uint64_t M, uint64_t, uint64_t K) { return M <= thc::kFp8NarrowRows && K != 0; }
+static bool linear_in_one_launch(uint64_t M, uint64_t N, uint64_t K) { return K != 0 && thc::fp8_product_is_direct(M, N, K); }
 
 // The workspace of thc_fp8_linear: the codes of x, its scales, the product's own workspace.
 uint64_t thc_fp8_linear_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
-    if (!fp8_product_in_range(M, N, K) || M == 0 || N == 0 || linear_in_one_launch(M, N, K)) return 0;
+    if (!fp8_product_in_range(M, N, K) || M == 0 || N == 0) return 0;
+    if (linear_in_one_launch(M, N, K)) return thc::fp8_matmul_workspace_bytes(M, N, K);
     return M * thc::fp8_row_bytes(K) + round16(4 * thc::fp8_scale_words(M, K)) + thc::fp8_matmul_workspace_bytes(M, N, K);
 }
 
@@ -1237,7 +1239,7 @@ int thc_fp8_linear(const void* x, thc_dtype dt, uint64_t M, uint64_t K, uint64_t
         (need != 0 && !aligned(workspace, 16)))
         return THC_ERR_ALIGN;
     if (linear_in_one_launch(M, N, K)) {
-        thc::Fp8NarrowArgs a{};
+        thc::Fp8DirectArgs a{};
         a.x = x;
         a.ldx = ldx;
         a.source = dt == THC_BF16 ? 1 : 2;
@@ -1251,7 +1253,8 @@ int thc_fp8_linear(const void* x, thc_dtype dt, uint64_t M, uint64_t K, uint64_t
         a.out_bf16 = out_dt == THC_BF16;
         a.c = out;
         a.ldc = ldo;
-        return finish(thc::launch_fp8_narrow(a, static_cast<hipStream_t>(stream)));
+        a.workspace = static_cast<float*>(workspace);
+        return finish(thc::launch_fp8_direct(a, static_cast<hipStream_t>(stream)));
     }
     uint8_t* codes = static_cast<uint8_t*>(workspace);
     uint8_t* scales = codes + M * thc::fp8_row_bytes(K);

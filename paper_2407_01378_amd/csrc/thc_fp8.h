@@ -15,6 +15,15 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+// 16 bytes at an address of any alignment that the element type has: the hardware takes them in one access.
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef words4 words4_any __attribute__((aligned(2)));
+__device__ __forceinline__ uint4 load16(const void* p) {
+    const words4 v = *static_cast<const words4_any*>(p);
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store16(void* p, uint4 v) { *static_cast<words4_any*>(p) = words4{v.x, v.y, v.z, v.w}; }
+
 // The scale byte of a block whose largest magnitude has these fp32 bits: the smallest e >= 0 with
 // amax <= 1.75 * 2^TOP * 2^(e - 127), where 1.75 * 2^TOP is the format's largest value (448 or 57344).
 template <bool E5M2>
@@ -126,13 +135,13 @@ __device__ __forceinline__ f32x16 fp8_mfma32(i32x8 a, i32x8 b, f32x16 d, uint32_
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, d, FA, FB, 0, (int)scale_a, 0, (int)scale_b);
 }
 
-// 8 neighbouring values of a row of C, on the 16-byte grid.
+// 8 neighbouring values of a row.
 template <bool BF16>
 struct Row8 {
     uint4 w[BF16 ? 1 : 2];
     __device__ __forceinline__ void load(const void* c) {
 #pragma unroll
-        for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = static_cast<const uint4*>(c)[i];
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = load16(static_cast<const uint4*>(c) + i);
     }
     __device__ __forceinline__ void add_to(float (&v)[8]) const {
         const uint32_t x[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[BF16 ? 0 : 1].x, w[BF16 ? 0 : 1].y, w[BF16 ? 0 : 1].z, w[BF16 ? 0 : 1].w};
@@ -142,10 +151,12 @@ struct Row8 {
     }
     static __device__ __forceinline__ void store(void* c, const float (&v)[8]) {
         if (BF16) {
-            *static_cast<uint4*>(c) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+            store16(c, make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])));
         } else {
-            static_cast<float4*>(c)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            static_cast<float4*>(c)[1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                store16(static_cast<uint4*>(c) + i, make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                                               __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
         }
     }
 };
@@ -159,6 +170,34 @@ __device__ __forceinline__ void store1(void* c, float v, bool accumulate) {
         float* p = static_cast<float*>(c);
         *p = accumulate ? v + *p : v;
     }
+}
+
+// `left` (at least 1) of 4 neighbouring values of a row.
+template <bool BF16>
+__device__ __forceinline__ void store4(void* c, const f32x4& v, uint32_t left, bool accumulate) {
+    if (left >= 4u && !accumulate) {
+        if (BF16) {
+            typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+            *static_cast<u32x2_any*>(c) = u32x2_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+        } else {
+            store16(c, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+        }
+        return;
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 4u; ++e)
+        if (e < left) store1<BF16>(static_cast<uint8_t*>(c) + e * (BF16 ? 2u : 4u), v[e], accumulate);
+}
+
+// The place of workgroup `id` among `total` tiles: workgroups go round the 8 dies in turn, and each die's workgroups take a
+// contiguous run of tiles, in columns of 4 tiles in m, so that what a die reads at a time is few rows of A and B.
+__device__ __forceinline__ void place_tile(uint32_t id, uint32_t total, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
+    const uint32_t die = id & 7u, of_die = id >> 3, share = total >> 3, rest = total & 7u;
+    const uint32_t t = die * share + (die < rest ? die : rest) + of_die;
+    const uint32_t group = t / (4u * tiles_n), first = group * 4u, high = tiles_m - first < 4u ? tiles_m - first : 4u;
+    const uint32_t in_group = t - group * 4u * tiles_n;
+    tm = first + in_group % high;
+    tn = in_group / high;
 }
 
 }  // namespace thc

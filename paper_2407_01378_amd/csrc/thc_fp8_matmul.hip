@@ -1,8 +1,8 @@
 // C = A B^T of two 8-bit matrices with a power-of-two scale for each block of 128 along k.
 //
-// Tiled form: a workgroup of 4 waves takes BM x BN of C and walks along k in steps of 128, one block of scales.  A step's
-// codes go from memory to LDS without passing registers, two steps deep; each wave multiplies (BM / 2) x (BN / 2) with
-// 32 x 32 matrix instructions while the codes of the next half step are read from LDS.
+// A workgroup of 4 waves takes 256 x 256 or 128 x 128 of C and walks along k in steps of 128, one block of scales.  A step's
+// codes go from memory to LDS without passing registers, up to two and a half steps ahead; each wave multiplies a
+// quarter of the tile with 32 x 32 matrix instructions while the codes of the next half step are read from LDS.
 #include "thc_fp8.h"
 #include "thc_internal.h"
 
@@ -16,19 +16,8 @@ constexpr uint64_t kMaxGrid = 1ull << 23;   // workgroups of 256 threads: 2^31 t
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-// The place of workgroup `id` among `total` tiles: workgroups go round the 8 dies in turn, and each die's workgroups take a
-// contiguous run of tiles, in columns of 4 tiles in m, so that what a die reads at a time is few rows of A and B.
-__device__ __forceinline__ void place_tile(uint32_t id, uint32_t total, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
-    const uint32_t die = id & 7u, of_die = id >> 3, share = total >> 3, rest = total & 7u;
-    const uint32_t t = die * share + (die < rest ? die : rest) + of_die;
-    const uint32_t group = t / (4u * tiles_n), first = group * 4u, high = tiles_m - first < 4u ? tiles_m - first : 4u;
-    const uint32_t in_group = t - group * 4u * tiles_n;
-    tm = first + in_group % high;
-    tn = in_group / high;
-}
-
 template <int FA, int FB, bool EXACT, int MF, int NF>
-__global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n, bool vector) {
+__global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n) {
     constexpr uint32_t BM = 64u * MF, BN = 64u * NF;
     static_assert(MF == NF, "the four units of a step have one size");
     // A step's codes are four units, the even and the odd halves of the waves' rows of A and of B; ten units fit LDS.  (Arrays of
@@ -41,7 +30,10 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     const uint32_t x = lane & 31u, h = lane >> 5, wm = wave & 1u, wn = wave >> 1;
     uint32_t tm, tn;
     place_tile(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
-    const uint32_t m0 = tm * BM, n0 = tn * BN, steps = (a.K + kStep - 1u) / kStep, ld = steps * kStep;
+    // this workgroup's part of the blocks along k
+    const uint32_t blocks = (a.K + kStep - 1u) / kStep, ld = blocks * kStep, first = blockIdx.y * a.share;
+    const uint32_t steps = blocks - first < a.share ? blocks - first : a.share;
+    const uint32_t m0 = tm * BM, n0 = tn * BN;
 
     // memory -> LDS: a wave moves 8 rows (whole lines of memory) at a time, lane l the piece of 16 codes that belongs at place
     // l % 8 of row l / 8.  Piece c of a row lies at place c ^ key: two rows fill all banks, and of 16 lanes that read
@@ -68,7 +60,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     auto fetch = [&](uint8_t* s, auto unit, uint32_t step) {
         constexpr uint32_t u = decltype(unit)::value;
         asm volatile("" : "+s"(base));   // (all places in LDS, kept across the loop, would not fit the scalar registers)
-        const int k = (int)(step < steps ? step * kStep : 0u);   // (behind the last step: not used)
+        const int k = (int)((first + (step < steps ? step : 0u)) * kStep);   // (behind the last step: not used)
 #pragma unroll
         for (uint32_t i = 0; i < MF; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(u < 2u ? src_a : src_b, (lds_void*)(s + base + i * 4096u), 16, (int)off[u][i], k, 0, 0);
@@ -114,7 +106,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         for (uint32_t f = 0; f < NF; ++f) wb[f] = *reinterpret_cast<const uint32_t*>(pb + row_b[f]);
     };
 
-    const uint32_t words = (steps + 3u) / 4u;
+    const uint32_t word0 = first >> 2, words = (blocks + 3u) / 4u;
     uint32_t sa[MF], sb[NF], next_a[MF], next_b[NF];
     f32x16 acc[MF][NF];
 #pragma unroll
@@ -197,12 +189,12 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         fetch(slots[(u + 11u) % kSlots], std::integral_constant<uint32_t, 3>{}, k + 2u);
         multiply(fa1, fb1);
         order();
-        if ((k & 3u) == 3u) {   // (moved, not renamed: a load that may be on its way would be waited for in every step)
+        if (((first + k) & 3u) == 3u) {   // (moved, not renamed: a load that may be on its way would be waited for in every step)
 #pragma unroll
             for (int i = 0; i < MF; ++i) asm volatile("v_mov_b32 %0, %1" : "=v"(sa[i]) : "v"(next_a[i]));
 #pragma unroll
             for (int j = 0; j < NF; ++j) asm volatile("v_mov_b32 %0, %1" : "=v"(sb[j]) : "v"(next_b[j]));
-            const uint32_t w = (k >> 2) + 2u;
+            const uint32_t w = ((first + k) >> 2) + 2u;
             scales(w < words ? w : 0u, next_a, next_b);
         } else {
 #pragma unroll
@@ -211,8 +203,12 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
             for (int j = 0; j < NF; ++j) sb[j] >>= 8;
         }
     };
-    scales(0, sa, sb);
-    scales(words > 1u ? 1u : 0u, next_a, next_b);
+    scales(word0, sa, sb);
+    scales(word0 + 1u < words ? word0 + 1u : 0u, next_a, next_b);
+#pragma unroll
+    for (int i = 0; i < MF; ++i) sa[i] >>= 8u * (first & 3u);
+#pragma unroll
+    for (int j = 0; j < NF; ++j) sb[j] >>= 8u * (first & 3u);
     fetch(s0, std::integral_constant<uint32_t, 0>{}, 0);
     fetch(s1, std::integral_constant<uint32_t, 1>{}, 0);
     fetch(s2, std::integral_constant<uint32_t, 2>{}, 0);
@@ -241,78 +237,62 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     if (k + 3u < steps) step(std::integral_constant<uint32_t, 3>{}, k + 3u);
     __builtin_amdgcn_s_waitcnt(0x0F70);   // (what was fetched behind the last step)
 
+    // 32 rows' sums at a time out of the matrix unit's registers, 8 neighbouring ones a lane.  One of several parts keeps its
+    // sums as they are, in rows with room up to a multiple of 8.
     constexpr bool BF16 = !EXACT;
-    constexpr uint32_t kSize = BF16 ? 2u : 4u, kCols = 32u * NF;
-    const uint32_t mw = m0 + wm * 32u * MF, nw = n0 + wn * kCols;
-    uint8_t* c = static_cast<uint8_t*>(a.c);
-    if (vector && n0 + BN <= a.N) {
-        // A whole tile with rows on the 16-byte grid: straight from the registers.
-        auto rows = [&](auto add) {
-#pragma unroll
-            for (uint32_t i = 0; i < MF; ++i) {
-                const uint32_t m = mw + i * 32u + x;
-                if (m >= a.M) continue;
-                uint8_t* at = c + ((uint64_t)m * a.ldc + nw + 8u * h) * kSize;
-                Row8<BF16> old[NF][2];
-                if (decltype(add)::value) {
-#pragma unroll
-                    for (uint32_t j = 0; j < 2u * NF; ++j) old[j >> 1][j & 1u].load(at + j * 16u * kSize);
-                }
-#pragma unroll
-                for (uint32_t j = 0; j < 2u * NF; ++j) {
-                    float v[8];
-#pragma unroll
-                    for (uint32_t e = 0; e < 8u; ++e) v[e] = acc[i][j >> 1][8u * (j & 1u) + e];
-                    if (decltype(add)::value) old[j >> 1][j & 1u].add_to(v);
-                    Row8<BF16>::store(at + j * 16u * kSize, v);
-                }
-            }
-        };
-        if (a.accumulate) rows(std::true_type{});
-        else rows(std::false_type{});
-        return;
-    }
-    // Otherwise by way of LDS, 32 rows of a wave at a time, so that neighbouring lanes store neighbouring values.
-    __builtin_amdgcn_s_barrier();
-    if (nw >= a.N) return;
-    // (two units to a strip, one behind the other)
-    constexpr uint32_t kPitch = kCols + 4u, kHalfRows = 16u;
-    static_assert(kHalfRows * kPitch * sizeof(float) <= kUnit, "half a strip fits a unit");
-    float* const lower = reinterpret_cast<float*>(wave == 0u ? s0 : wave == 1u ? s1 : wave == 2u ? s2 : s3);
-    float* const upper = reinterpret_cast<float*>(wave == 0u ? s4 : wave == 1u ? s5 : wave == 2u ? s6 : s7);
-    auto strip = [&](uint32_t r) { return (r < kHalfRows ? lower : upper) + (r % kHalfRows) * kPitch; };
-    const uint32_t cols = a.N - nw < kCols ? a.N - nw : kCols;
+    constexpr uint32_t kSize = BF16 ? 2u : 4u;
+    const bool part = a.share < blocks, add = a.accumulate && !part;
+    const uint64_t pitch = fp8_part_pitch(a.N);
+    float* sums = a.workspace + blockIdx.y * a.M * pitch;
+    const uint32_t n = n0 + wn * 32u * NF + 8u * h;
 #pragma unroll
     for (uint32_t i = 0; i < MF; ++i) {
+        const uint32_t m = m0 + wm * 32u * MF + i * 32u + x;
+        __builtin_amdgcn_sched_barrier(0);
+        if (m >= a.M) continue;
+        uint8_t* at = static_cast<uint8_t*>(a.c) + ((uint64_t)m * a.ldc + n) * kSize;
+        Row8<BF16> old[2 * NF] = {};
+        if (add) {
 #pragma unroll
-        for (uint32_t j = 0; j < NF; ++j)
-#pragma unroll
-            for (uint32_t q = 0; q < 4u; ++q) {
-                float* at = strip(x) + j * 32u + 16u * (q >> 1) + 8u * h + 4u * (q & 1u);
-                *reinterpret_cast<float4*>(at) = make_float4(acc[i][j][4u * q], acc[i][j][4u * q + 1u], acc[i][j][4u * q + 2u], acc[i][j][4u * q + 3u]);
-            }
-        const uint32_t m1 = mw + i * 32u, rows = m1 >= a.M ? 0u : a.M - m1 < 32u ? a.M - m1 : 32u;
-        if (BF16 && !a.accumulate) {
-            // pairs on the 4-byte grid, then the values left over at a row's ends
-#pragma unroll 4
-            for (uint32_t r = 0; r < rows; ++r) {
-                uint8_t* at = c + ((uint64_t)(m1 + r) * a.ldc + nw) * 2u;
-                const uint32_t n = 2u * lane + (uint32_t)(reinterpret_cast<uintptr_t>(at) >> 1 & 1u);
-                if (n + 1u < cols) *reinterpret_cast<uint32_t*>(at + 2u * n) = bf16_pair(strip(r)[n], strip(r)[n + 1u]);
-            }
-            const uint32_t r = lane >> 1;
-            if (r < rows) {
-                uint8_t* at = c + ((uint64_t)(m1 + r) * a.ldc + nw) * 2u;
-                const uint32_t odd = (uint32_t)(reinterpret_cast<uintptr_t>(at) >> 1 & 1u), n = lane & 1u ? cols - 1u : 0u;
-                if (lane & 1u ? ((cols - odd) & 1u) != 0u && n >= odd : odd != 0u) store1<true>(at + 2u * n, strip(r)[n], false);
-            }
-        } else {
-#pragma unroll 2
-            for (uint32_t r = 0; r < rows; ++r)
-#pragma unroll
-                for (uint32_t n = lane; n < kCols; n += 64u)
-                    if (n < cols) store1<BF16>(c + ((uint64_t)(m1 + r) * a.ldc + nw + n) * kSize, strip(r)[n], a.accumulate);
+            for (uint32_t j = 0; j < 2u * NF; ++j)
+                if (n + 16u * j + 8u <= a.N) old[j].load(at + j * 16u * kSize);
         }
+#pragma unroll
+        for (uint32_t j = 0; j < 2u * NF; ++j) {
+            const uint32_t nj = n + 16u * j;
+            float v[8];
+#pragma unroll
+            for (uint32_t e = 0; e < 8u; ++e) v[e] = acc[i][j >> 1][8u * (j & 1u) + e];
+            if (part) {
+                if (nj < a.N) Row8<false>::store(sums + m * pitch + nj, v);
+            } else if (nj + 8u <= a.N) {
+                if (add) old[j].add_to(v);
+                Row8<BF16>::store(at + j * 16u * kSize, v);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 7u; ++e)
+                    if (nj + e < a.N) store1<BF16>(at + (j * 16u + e) * kSize, v[e], add);
+            }
+        }
+    }
+}
+
+// The parts' sums, added in their order: four neighbouring values of a row to a thread.
+template <bool BF16>
+__global__ __launch_bounds__(256) void fp8_join_kernel(Fp8MatmulArgs a, uint32_t parts) {
+    const uint32_t pieces = (a.N + 3u) / 4u;
+    const uint64_t pitch = fp8_part_pitch(a.N), total = (uint64_t)a.M * pieces, step = (uint64_t)gridDim.x * 256u;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < total; i += step) {
+        const uint32_t m = (uint32_t)(i / pieces), n = (uint32_t)(i % pieces) * 4u;
+        const float* at = a.workspace + m * pitch + n;
+        float4 v = *reinterpret_cast<const float4*>(at);
+#pragma unroll 4
+        for (uint32_t p = 1; p < parts; ++p) {
+            const float4 w = *reinterpret_cast<const float4*>(at + p * a.M * pitch);
+            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+        }
+        uint8_t* c = static_cast<uint8_t*>(a.c) + (m * a.ldc + n) * (BF16 ? 2u : 4u);
+        store4<BF16>(c, f32x4{v.x, v.y, v.z, v.w}, a.N - n, a.accumulate);
     }
 }
 
@@ -328,34 +308,96 @@ __global__ __launch_bounds__(256) void zero_matrix_kernel(Fp8MatmulArgs a) {
 
 }  // namespace
 
-uint64_t fp8_matmul_workspace_bytes(uint64_t, uint64_t, uint64_t) { return 0; }
+// How a product is done, by its sizes alone (an order of additions may depend on nothing else).  Measured on the device:
+//  - up to 16 rows: direct, unless there are 24576 rows of B or more (one row, 2048 along k: 8192 rows of B 7.5 us direct and
+//    10.6 us tiled, 50257 rows 41 and 21 us);
+//  - tiles of 256 x 256 from 160 of them on, three out of five compute units (2048 x 4096 x 2048, 128 tiles: 28 us, and 20 us in
+//    tiles of 128 x 128; 3000 x 4096 x 2048, 192 tiles: 31 and 30 us; 4096^3, 256 tiles: 55 and 67 us);
+//  - short products of few tiles of 128 x 128: direct, tiles of 64 x 64 (777 x 520 x 1000, 35 tiles: 8.1 and 12 us;
+//    1024^3, 64 tiles: 8.0 and 6.7 us; 64 x 2048 x 2048, 16 tiles of 16 blocks each: 11.5 and 8.8 us);
+//  - tiles of 128 x 128 otherwise, the blocks along k divided among workgroups where that is expected to be
+//    shorter: a block takes such a tile 0.45 us, a second launch 2 us, and the parts' sums pass memory twice at about 3 TB/s
+//    (1024 x 1024 x 16384: 59 us undivided, 41, 29 and 31 us in 2, 4 and 8 parts; 512 x 2048 x 2048: 11, 15 and 20 us in 1, 2
+//    and 4 parts).
+struct Plan {
+    uint32_t tile;      // of the tiled kernel: 256 or 128; of the direct one: 64 or 16 (rows)
+    uint32_t parts;     // among which the blocks along k are divided
+};
+static Plan plan_for(uint64_t M, uint64_t N, uint64_t K) {
+    auto tiles = [&](uint64_t rows, uint64_t cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
+    const uint64_t steps = (K + kStep - 1) / kStep;
+    if (M <= kFp8FewRows && N < 24576u) {
+        uint64_t parts = 256u / tiles(16, 16);   // (no part shorter than two blocks for each of 8 waves)
+        parts = parts < steps / 16u ? parts : steps / 16u;
+        return {16u, (uint32_t)(parts > 1u ? parts : 1u)};
+    }
+    if (tiles(256, 256) >= 160u) return {256u, 1u};
+    const uint64_t count = tiles(128, 128);
+    if (count < 48u && tiles(64, 64) >= 40u && steps <= 12u) return {64u, 1u};
+    Plan best{128u, 1u};
+    double least = 0.45 * steps;
+    for (uint32_t parts = 2; parts * count <= 512u && parts * 4u <= steps; parts *= 2u) {
+        const double time = 0.45 * ((steps + parts - 1u) / parts) + 2.0 + 8e-6 / 3.0 * parts * M * fp8_part_pitch(N);
+        if (time < least) {
+            least = time;
+            best.parts = parts;
+        }
+    }
+    return best;
+}
 
-hipError_t launch_fp8_matmul(const Fp8MatmulArgs& a, hipStream_t stream) {
+bool fp8_product_is_direct(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K).tile == 16u; }
+
+uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
+    if (M == 0 || N == 0 || K == 0) return 0;
+    const Plan p = plan_for(M, N, K);
+    return p.parts > 1u ? p.parts * M * fp8_part_pitch(N) * sizeof(float) : 0;
+}
+
+uint32_t fp8_direct_parts(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K).parts; }
+
+hipError_t launch_fp8_matmul(const Fp8MatmulArgs& args, hipStream_t stream) {
+    Fp8MatmulArgs a = args;
     if (a.K == 0u) {   // (there may be no codes and scales to read)
         if (a.accumulate) return hipSuccess;
         const uint64_t blocks = ((uint64_t)a.M * a.N + 255u) / 256u;
         zero_matrix_kernel<<<(uint32_t)(blocks < 4096u ? blocks : 4096u), 256, 0, stream>>>(a);
         return hipGetLastError();
     }
-    if (a.M <= kFp8NarrowRows) {
-        Fp8NarrowArgs narrow{};
-        static_cast<Fp8MatmulArgs&>(narrow) = a;
-        return launch_fp8_narrow(narrow, stream);
+    const Plan plan = plan_for(a.M, a.N, a.K);
+    if (plan.tile < 128u) {
+        Fp8DirectArgs direct{};
+        static_cast<Fp8MatmulArgs&>(direct) = a;
+        return launch_fp8_direct(direct, stream);
     }
-    const uint32_t size = a.out_bf16 ? 2u : 4u;
-    const bool vector = (reinterpret_cast<uintptr_t>(a.c) & 15u) == 0 && a.ldc * size % 16u == 0;
-    auto go = [&](auto FA, auto FB) {
+    const uint32_t blocks = (a.K + kStep - 1u) / kStep;
+    const uint64_t tiles_m = (a.M + plan.tile - 1u) / plan.tile, tiles_n = (a.N + plan.tile - 1u) / plan.tile;
+    if (tiles_m * tiles_n > kMaxGrid) return hipErrorInvalidValue;
+    const uint32_t tm = (uint32_t)tiles_m, tn = (uint32_t)tiles_n;
+    a.share = (blocks + plan.parts - 1u) / plan.parts;
+    const uint32_t parts = (blocks + a.share - 1u) / a.share;
+    const dim3 grid(tm * tn, parts);
+    auto go = [&](auto FA, auto FB, auto EXACT) {
         constexpr int A = decltype(FA)::value, B = decltype(FB)::value;
-        const uint32_t tiles_m = (a.M + 255u) / 256u, tiles_n = (a.N + 255u) / 256u;
-        if ((uint64_t)tiles_m * tiles_n > kMaxGrid) return hipErrorInvalidValue;
-        if (a.out_bf16) fp8_matmul_tiled_kernel<A, B, false, 4, 4><<<tiles_m * tiles_n, 256, 0, stream>>>(a, tiles_m, tiles_n, vector);
-        else fp8_matmul_tiled_kernel<A, B, true, 4, 4><<<tiles_m * tiles_n, 256, 0, stream>>>(a, tiles_m, tiles_n, vector);
+        constexpr bool E = decltype(EXACT)::value;
+        if (plan.tile == 256u) fp8_matmul_tiled_kernel<A, B, E, 4, 4><<<grid, 256, 0, stream>>>(a, tm, tn);
+        else fp8_matmul_tiled_kernel<A, B, E, 2, 2><<<grid, 256, 0, stream>>>(a, tm, tn);
         return hipGetLastError();
     };
-    auto with_b = [&](auto FA) {
-        return a.b_e5m2 ? go(FA, std::integral_constant<int, 1>{}) : go(FA, std::integral_constant<int, 0>{});
-    };
-    return a.a_e5m2 ? with_b(std::integral_constant<int, 1>{}) : with_b(std::integral_constant<int, 0>{});
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    auto out = [&](auto FA, auto FB) { return a.out_bf16 ? go(FA, FB, std::false_type{}) : go(FA, FB, std::true_type{}); };
+    auto with_b = [&](auto FA) { return a.b_e5m2 ? out(FA, I1{}) : out(FA, I0{}); };
+    const hipError_t rc = a.a_e5m2 ? with_b(I1{}) : with_b(I0{});
+    return rc != hipSuccess || parts == 1u ? rc : launch_fp8_join(a, parts, stream);
+}
+
+hipError_t launch_fp8_join(const Fp8MatmulArgs& a, uint32_t parts, hipStream_t stream) {
+    const uint64_t join = ((uint64_t)a.M * ((a.N + 3u) / 4u) + 255u) / 256u;
+    const uint32_t join_grid = (uint32_t)(join < 4096u ? join : 4096u);
+    if (a.out_bf16) fp8_join_kernel<true><<<join_grid, 256, 0, stream>>>(a, parts);
+    else fp8_join_kernel<false><<<join_grid, 256, 0, stream>>>(a, parts);
+    return hipGetLastError();
 }
 
 }  // namespace thc

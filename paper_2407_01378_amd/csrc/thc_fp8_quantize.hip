@@ -29,22 +29,27 @@ __device__ __forceinline__ uint32_t row16_umax(uint32_t x) {
     return x;
 }
 
+// 8 neighbouring values, of which `valid` exist.
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* x, uint64_t at, uint32_t valid, bool vector, float (&v)[8]) {
-    if (vector && valid >= 8u) {
+__device__ __forceinline__ void load8(const void* x, uint64_t at, uint32_t valid, float (&v)[8]) {
+    if (valid >= 8u) {
         if (BF16) {
-            const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + at);
+            const uint4 q = load16(static_cast<const uint16_t*>(x) + at);
             const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                v[2 * d] = __uint_as_float(w[d] << 16);
-                v[2 * d + 1] = __uint_as_float(w[d] & 0xFFFF0000u);
+                v[2 * d] = bf16_low(w[d]);
+                v[2 * d + 1] = bf16_high(w[d]);
             }
         } else {
-            const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(x) + at);
-            const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(x) + at + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                const uint4 q = load16(static_cast<const float*>(x) + at + 4 * d);
+                v[4 * d] = __uint_as_float(q.x);
+                v[4 * d + 1] = __uint_as_float(q.y);
+                v[4 * d + 2] = __uint_as_float(q.z);
+                v[4 * d + 3] = __uint_as_float(q.w);
+            }
         }
         return;
     }
@@ -52,8 +57,7 @@ __device__ __forceinline__ void load8(const void* x, uint64_t at, uint32_t valid
     for (uint32_t e = 0; e < 8u; ++e) {
         float f = 0.0f;
         if (e < valid)
-            f = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(x)[at + e] << 16)
-                     : static_cast<const float*>(x)[at + e];
+            f = BF16 ? bf16_low(static_cast<const uint16_t*>(x)[at + e]) : static_cast<const float*>(x)[at + e];
         v[e] = f;
     }
 }
@@ -69,7 +73,7 @@ __device__ __forceinline__ void store_scale(uint32_t* scales, uint32_t rows, uin
 }
 
 template <bool BF16, bool E5M2, bool TILE>
-__global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs a, uint32_t tiles_c, uint64_t tiles, bool vector) {
+__global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs a, uint32_t tiles_c, uint64_t tiles) {
     __shared__ uint32_t s_max[16][kTile];
     __shared__ uint2 s_code[kTile][16];
     __shared__ uint32_t s_row[kTile], s_col[kTile];
@@ -84,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs 
 #pragma unroll
         for (uint32_t p = 0; p < 8u; ++p) {
             const uint32_t r = r0 + p, valid = r < a.rows && c0 < a.cols ? a.cols - c0 : 0u;
-            load8<BF16>(a.x, (uint64_t)r * a.ld + c0, valid, vector, v[p]);
+            load8<BF16>(a.x, (uint64_t)r * a.ld + c0, valid, v[p]);
         }
         uint32_t rm[8], cm[8];
 #pragma unroll
@@ -174,11 +178,40 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs 
     }
 }
 
+// Along the rows only: 16 lanes take a block, a wave 4 neighbouring blocks of a row, which share their scale word.
+template <bool BF16, bool E5M2>
+__global__ __launch_bounds__(kThreads) void fp8_quantize_rows_kernel(Fp8QuantizeArgs a, uint32_t groups, uint64_t total) {
+    const uint32_t lane = threadIdx.x & 63u, cg = lane & 15u, blocks = (a.cols + 127u) / 128u;
+    const uint64_t q_ld = (uint64_t)blocks * 128u, step = (uint64_t)gridDim.x * (kThreads / 64u);
+    for (uint64_t i = (uint64_t)blockIdx.x * (kThreads / 64u) + (threadIdx.x >> 6); i < total; i += step) {
+        const uint32_t r = (uint32_t)(i / groups), group = (uint32_t)(i % groups), j = 4u * group + (lane >> 4), c = j * 128u + cg * 8u;
+        float v[8];
+        load8<BF16>(a.x, (uint64_t)r * a.ld + c, c < a.cols ? a.cols - c : 0u, v);
+        uint32_t m = 0u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t y = magnitude(v[e]);
+            m = y > m ? y : m;
+        }
+        m = row16_umax(m);
+        const uint32_t e = fp8_scale_byte<E5M2>(m);
+        const float scale = fp8_scale(e);
+        uint2 w;
+        w.x = fp8_codes<E5M2>(v[0], v[1], v[2], v[3], scale);
+        w.y = fp8_codes<E5M2>(v[4], v[5], v[6], v[7], scale);
+        if (e == 255u) w.x = w.y = 0x7F7F7F7Fu;
+        if (j < blocks) *reinterpret_cast<uint2*>(a.q + r * q_ld + c) = w;   // (behind the last block: zeros, and scale 0)
+        uint32_t word = e << (8u * (lane >> 4));
+        word |= (uint32_t)__shfl_xor((int)word, 16);
+        word |= (uint32_t)__shfl_xor((int)word, 32);
+        if (lane == 0u) a.scales[(uint64_t)group * a.rows + r] = word;
+    }
+}
+
 // 16 codes a thread.
 template <bool E5M2, bool BF16OUT>
 __global__ __launch_bounds__(kThreads) void fp8_dequantize_kernel(const uint8_t* q, const uint32_t* scales, uint32_t rows,
-                                                                  uint32_t cols, uint32_t pieces, void* out, uint64_t ld,
-                                                                  bool vector) {
+                                                                  uint32_t cols, uint32_t pieces, void* out, uint64_t ld) {
     const uint64_t total = (uint64_t)rows * pieces, step = (uint64_t)gridDim.x * kThreads;
     const uint64_t q_ld = (cols + 127u) / 128u * 128u;
     for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
@@ -195,20 +228,12 @@ __global__ __launch_bounds__(kThreads) void fp8_dequantize_kernel(const uint8_t*
         }
 #pragma unroll
         for (int k = 0; k < 16; ++k) v[k] = e == 255u ? __uint_as_float(0x7FC00000u) : ldexpf(v[k], (int)e - 127);
-        if (vector && c + 16u <= cols) {
-            if (BF16OUT) {
-                uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + (uint64_t)r * ld + c);
+        if (c + 16u <= cols) {
+            uint8_t* o = static_cast<uint8_t*>(out) + ((uint64_t)r * ld + c) * (BF16OUT ? 2u : 4u);
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    uint32_t p[4];
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) p[d] = bf16_pair(v[8 * k + 2 * d], v[8 * k + 2 * d + 1]);
-                    o[k] = make_uint4(p[0], p[1], p[2], p[3]);
-                }
-            } else {
-                float4* o = reinterpret_cast<float4*>(static_cast<float*>(out) + (uint64_t)r * ld + c);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            for (int k = 0; k < 2; ++k) {
+                const float half[8] = {v[8 * k], v[8 * k + 1], v[8 * k + 2], v[8 * k + 3], v[8 * k + 4], v[8 * k + 5], v[8 * k + 6], v[8 * k + 7]};
+                Row8<BF16OUT>::store(o + k * (BF16OUT ? 16 : 32), half);
             }
             continue;
         }
@@ -224,17 +249,25 @@ __global__ __launch_bounds__(kThreads) void fp8_dequantize_kernel(const uint8_t*
 
 uint32_t grid_for(uint64_t blocks) { return (uint32_t)(blocks < (1u << 20) ? blocks : (1u << 20)); }
 
-bool vector_rows(const void* p, uint64_t ld, uint32_t size) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * size % 16u == 0; }
-
 }  // namespace
 
 hipError_t launch_fp8_quantize(const Fp8QuantizeArgs& a, bool bf16, bool e5m2, bool tile, hipStream_t stream) {
     const uint32_t tiles_c = (uint32_t)(fp8_row_bytes(a.cols) / kTile);
     const uint64_t tiles = (uint64_t)tiles_c * (fp8_row_bytes(a.rows) / kTile);
-    const bool vector = vector_rows(a.x, a.ld, bf16 ? 2 : 4);
+    if (!a.q_t && !tile) {
+        const uint32_t groups = (a.cols + 511u) / 512u;
+        const uint64_t total = (uint64_t)a.rows * groups;
+        const uint32_t grid = grid_for((total + kThreads / 64u - 1u) / (kThreads / 64u));
+        auto rows = [&](auto B, auto E) {
+            fp8_quantize_rows_kernel<decltype(B)::value, decltype(E)::value><<<grid, kThreads, 0, stream>>>(a, groups, total);
+        };
+        auto with_format = [&](auto B) { e5m2 ? rows(B, std::true_type{}) : rows(B, std::false_type{}); };
+        bf16 ? with_format(std::true_type{}) : with_format(std::false_type{});
+        return hipGetLastError();
+    }
     auto go = [&](auto B, auto E, auto T) {
         fp8_quantize_kernel<decltype(B)::value, decltype(E)::value, decltype(T)::value>
-            <<<grid_for(tiles), kThreads, 0, stream>>>(a, tiles_c, tiles, vector);
+            <<<grid_for(tiles), kThreads, 0, stream>>>(a, tiles_c, tiles);
     };
     auto with_tile = [&](auto B, auto E) { tile ? go(B, E, std::true_type{}) : go(B, E, std::false_type{}); };
     auto with_format = [&](auto B) { e5m2 ? with_tile(B, std::true_type{}) : with_tile(B, std::false_type{}); };
@@ -246,10 +279,9 @@ hipError_t launch_fp8_dequantize(const uint8_t* q, const uint32_t* scales, bool 
                                  bool out_bf16, void* out, uint64_t ld, hipStream_t stream) {
     const uint32_t pieces = (cols + 15u) / 16u;
     const uint32_t grid = grid_for(((uint64_t)rows * pieces + kThreads - 1u) / kThreads);
-    const bool vector = vector_rows(out, ld, out_bf16 ? 2 : 4);
     auto go = [&](auto E, auto B) {
         fp8_dequantize_kernel<decltype(E)::value, decltype(B)::value>
-            <<<grid, kThreads, 0, stream>>>(q, scales, rows, cols, pieces, out, ld, vector);
+            <<<grid, kThreads, 0, stream>>>(q, scales, rows, cols, pieces, out, ld);
     };
     auto with_out = [&](auto E) { out_bf16 ? go(E, std::true_type{}) : go(E, std::false_type{}); };
     e5m2 ? with_out(std::true_type{}) : with_out(std::false_type{});

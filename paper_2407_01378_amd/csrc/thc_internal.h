@@ -253,18 +253,25 @@ struct Fp8MatmulArgs {
     uint32_t a_e5m2, b_e5m2, accumulate, out_bf16;
     void* c;
     uint64_t ldc;
-    float* workspace;
+    float* workspace;     // parts x M x fp8_part_pitch(N), where the blocks along k are divided
+    uint32_t share;       // blocks of one part, set by the launch
 };
+inline __host__ __device__ uint64_t fp8_part_pitch(uint64_t N) { return (N + 7) / 8 * 8; }
 uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
 hipError_t launch_fp8_matmul(const Fp8MatmulArgs& a, hipStream_t stream);
-// Few rows of A, given as codes (source 0) or as values to be quantized on the way (1 = bf16, 2 = fp32); K > 0.
-constexpr uint32_t kFp8NarrowRows = 32;
-struct Fp8NarrowArgs : Fp8MatmulArgs {
+// The sum of the parts in a.workspace, in their order, to a.c.
+hipError_t launch_fp8_join(const Fp8MatmulArgs& a, uint32_t parts, hipStream_t stream);
+// Operands straight from memory, K > 0: tiles of 64 x 64, or, up to kFp8FewRows rows, 16 rows of B to a workgroup; there A is
+// given as codes (source 0) or as values to be quantized on the way (1 = bf16, 2 = fp32).
+constexpr uint32_t kFp8FewRows = 16;
+struct Fp8DirectArgs : Fp8MatmulArgs {
     const void* x;
     uint64_t ldx;
     uint32_t source;
 };
-hipError_t launch_fp8_narrow(const Fp8NarrowArgs& a, hipStream_t stream);
+bool fp8_product_is_direct(uint64_t M, uint64_t N, uint64_t K);   // few rows, and this is how thc_fp8_matmul does it
+uint32_t fp8_direct_parts(uint64_t M, uint64_t N, uint64_t K);
+hipError_t launch_fp8_direct(const Fp8DirectArgs& a, hipStream_t stream);
 
 // ---- embedding (thc_embed.hip) -----------------------------------------------------------------
 struct EmbedArgs {
