@@ -602,7 +602,7 @@ int thc_embed_forward(const void* table, thc_dtype dt, uint64_t vocab, uint64_t 
  *   grad_out     count x dim of type dt, ld
  *   grad_table   vocab x dim of out_dt, ldt
  *   workspace    thc_embed_backward_workspace_bytes(count, vocab, dim) bytes, 16-byte aligned
- * count, dim <= 2^31 - 1, vocab <= 2^31 - 1, count * dim < 2^44 (THC_ERR_SIZE). */
+ * count, vocab <= 2^31 - 1, dim <= 2^20, count * dim < 2^44 (THC_ERR_SIZE). */
 uint64_t thc_embed_backward_workspace_bytes(uint64_t count, uint64_t vocab, uint64_t dim);
 int thc_embed_backward(const void* grad_out, thc_dtype dt, uint64_t ld, const void* tokens, int index, uint64_t count,
                        uint64_t vocab, uint64_t dim, float scale, int accumulate, thc_dtype out_dt, void* grad_table,

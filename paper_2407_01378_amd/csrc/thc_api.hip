@@ -1296,7 +1296,7 @@ int thc_embed_forward(const void* table, thc_dtype dt, uint64_t vocab, uint64_t 
 }
 
 static bool embed_gradient_in_range(uint64_t count, uint64_t vocab, uint64_t dim) {
-    return count <= kMaxRows && vocab <= kMaxRows && dim <= kMaxRows && count * dim < kMaxCoords;
+    return count <= kMaxRows && vocab <= kMaxRows && dim <= (1ull << 20) && count * dim < kMaxCoords;
 }
 
 uint64_t thc_embed_backward_workspace_bytes(uint64_t count, uint64_t vocab, uint64_t dim) {

@@ -1,6 +1,12 @@
 // Embedding lookup and its gradient.
 //
-// Simple form of the gradient: a workgroup per row of the table looks through all tokens.
+// Lookup: rows are gathered 16 bytes a lane; memory is what bounds it.
+//
+// Gradient: the tokens are sorted (stable, so that a row's terms keep their order), the sorted list is cut into pieces of equal
+// length, and a group of lanes adds the rows of a piece, run by run of equal tokens: however often a token occurs,
+// the work is divided evenly, and every sum has one order.  A run inside a piece is written directly; of a run that
+// crosses a piece's border the piece keeps its part, and a last launch adds the parts.  Rows of the table whose token does not occur are
+// zeroed by further workgroups of the summing launch.  Where the whole gradient is written, that write is what bounds it.
 #include "thc_fp8.h"
 #include "thc_internal.h"
 
@@ -11,77 +17,488 @@ namespace {
 
 constexpr uint32_t kThreads = 256;
 
-__device__ __forceinline__ int64_t token_at(const EmbedArgs& a, uint32_t i) {
+// ---------------------------------------------------------------- values of a row, 8 a lane
+template <bool BF16>
+__device__ __forceinline__ void load_row(const void* p, uint64_t at, uint32_t valid, float (&v)[8]) {
+    if (valid >= 8u) {
+        Row8<BF16> r;
+        r.load(static_cast<const uint8_t*>(p) + at * (BF16 ? 2u : 4u));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+        r.add_to(v);
+        return;
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 8u; ++e)
+        v[e] = e >= valid ? 0.0f : BF16 ? bf16_low(static_cast<const uint16_t*>(p)[at + e]) : static_cast<const float*>(p)[at + e];
+}
+template <bool BF16>
+__device__ __forceinline__ void store_row(void* p, uint64_t at, uint32_t valid, const float (&v)[8]) {
+    uint8_t* c = static_cast<uint8_t*>(p) + at * (BF16 ? 2u : 4u);
+    if (valid >= 8u) {
+        Row8<BF16>::store(c, v);
+        return;
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 8u; ++e)
+        if (e < valid) store1<BF16>(c + e * (BF16 ? 2u : 4u), v[e], false);
+}
+
+__device__ __forceinline__ int64_t token_at(const EmbedArgs& a, uint64_t i) {
     return a.wide_tokens ? static_cast<const int64_t*>(a.tokens)[i] : (int64_t)static_cast<const int32_t*>(a.tokens)[i];
 }
-__device__ __forceinline__ float load1(const void* p, bool bf16, uint64_t at) {
-    return bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[at] << 16) : static_cast<const float*>(p)[at];
-}
-__device__ __forceinline__ void store1(void* p, bool bf16, uint64_t at, float v) {
-    if (bf16) static_cast<uint16_t*>(p)[at] = bf16_bits(v);
-    else static_cast<float*>(p)[at] = v;
-}
 
-__global__ __launch_bounds__(kThreads) void embed_forward_kernel(EmbedArgs a) {
-    for (uint32_t i = blockIdx.x; i < a.count; i += gridDim.x) {
-        const int64_t v = token_at(a, i);
-        const bool in = v >= 0 && v < (int64_t)a.vocab;
-        for (uint32_t d = threadIdx.x; d < a.dim; d += kThreads)
-            store1(a.out, a.out_bf16, (uint64_t)i * a.ld_out + d,
-                   in ? a.scale * load1(a.in, a.in_bf16, (uint64_t)v * a.ld_in + d) : 0.0f);
+// ---------------------------------------------------------------- lookup
+template <bool IN, bool OUT>
+__global__ __launch_bounds__(kThreads) void embed_forward_kernel(EmbedArgs a, uint32_t pieces) {
+    const uint64_t total = (uint64_t)a.count * pieces, step = (uint64_t)gridDim.x * kThreads;
+    for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
+        const uint64_t row = i / pieces;
+        const uint32_t d = (uint32_t)(i % pieces) * 8u, valid = a.dim - d;
+        const int64_t token = token_at(a, row);
+        float v[8] = {};
+        if (token >= 0 && token < (int64_t)a.vocab) {
+            load_row<IN>(a.in, (uint64_t)token * a.ld_in + d, valid, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+        }
+        store_row<OUT>(a.out, row * a.ld_out + d, valid, v);
     }
 }
 
-__global__ __launch_bounds__(kThreads) void embed_backward_simple_kernel(EmbedArgs a) {
-    __shared__ uint32_t s_found[kThreads];
-    __shared__ uint32_t s_count[kThreads / 64u];
+// ---------------------------------------------------------------- sorting the tokens
+// Keys: the token, or `vocab` for one outside the table, which sorts behind all others.
+__device__ __forceinline__ uint32_t key_at(const EmbedArgs& a, uint32_t i) {
+    const int64_t t = token_at(a, i);
+    return t >= 0 && t < (int64_t)a.vocab ? (uint32_t)t : a.vocab;
+}
+
+// Lanes that hold the same digit as this one, among those of `in`.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, uint32_t bits, uint64_t in) {
+    uint64_t mask = in;
+    for (uint32_t b = 0; b < bits; ++b) {
+        const bool one = (digit >> b) & 1u;
+        const uint64_t ones = __ballot(one);
+        mask &= one ? ones : ~ones;
+    }
+    return mask;
+}
+
+// Between the accesses of a wave's lanes to what other lanes of the wave have written in LDS.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// One pass of a stable radix sort.  The list is cut into at most 256 tiles, one per workgroup; `counts` holds every tile's number of keys per
+// digit.
+struct SortPass {
+    const uint32_t* keys;    // null: the tokens themselves, in their order
+    const uint32_t* places;
+    uint32_t* keys_out;
+    uint32_t* places_out;
+    uint32_t* counts;        // tiles x digits
+    uint32_t tile;           // keys of a tile, a multiple of 256
+    uint32_t shift, bits;
+};
+
+__global__ __launch_bounds__(kThreads) void sort_count_kernel(EmbedArgs a, SortPass s) {
+    extern __shared__ uint32_t s_count[];
+    const uint32_t digits = 1u << s.bits, first = blockIdx.x * s.tile, end = a.count - first < s.tile ? a.count : first + s.tile;
+    for (uint32_t d = threadIdx.x; d < digits; d += kThreads) s_count[d] = 0u;
+    __syncthreads();
+    for (uint32_t i = first + threadIdx.x; i < end; i += kThreads) {
+        const uint32_t key = s.keys ? s.keys[i] : key_at(a, i);
+        atomicAdd(&s_count[(key >> s.shift) & (digits - 1u)], 1u);
+    }
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < digits; d += kThreads) s.counts[(uint64_t)blockIdx.x * digits + d] = s_count[d];
+}
+
+// Sum of the values of lower threads.
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* s_wave) {
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6;
-    for (uint32_t v = blockIdx.x; v < a.vocab; v += gridDim.x) {
-        for (uint32_t d0 = 0; d0 < a.dim; d0 += kThreads) {
-            const uint32_t d = d0 + t;
-            float sum = 0.0f;
-            bool any = false;
-            for (uint64_t i0 = 0; i0 < a.count; i0 += kThreads) {
-                const uint64_t i = i0 + t;
-                const bool match = i < a.count && token_at(a, (uint32_t)i) == (int64_t)v;
-                const uint64_t mask = __ballot(match);
-                if (lane == 0u) s_count[wave] = __popcll(mask);
-                __syncthreads();
-                uint32_t before = 0, total = 0;
-                for (uint32_t w = 0; w < kThreads / 64u; ++w) {
-                    before += w < wave ? s_count[w] : 0u;
-                    total += s_count[w];
-                }
-                if (match) s_found[before + __popcll(mask & ((1ull << lane) - 1ull))] = (uint32_t)i;
-                __syncthreads();
-                any = any || total != 0u;
-                if (d < a.dim)
-                    for (uint32_t k = 0; k < total; ++k) sum += load1(a.in, a.in_bf16, (uint64_t)s_found[k] * a.ld_in + d);
-                __syncthreads();
-            }
-            if (d < a.dim && (any || !a.accumulate)) {
-                const uint64_t at = (uint64_t)v * a.ld_out + d;
-                float r = any ? sum * a.scale : 0.0f;
-                if (a.accumulate) r += load1(a.out, a.out_bf16, at);
-                store1(a.out, a.out_bf16, at, r);
-            }
+    uint32_t x = v;
+#pragma unroll
+    for (uint32_t o = 1; o < 64u; o <<= 1) {
+        const uint32_t y = (uint32_t)__shfl_up((int)x, o);
+        x += lane >= o ? y : 0u;
+    }
+    if (lane == 63u) s_wave[wave] = x;
+    __syncthreads();
+    uint32_t before = x - v;
+    for (uint32_t w = 0; w < wave; ++w) before += s_wave[w];
+    __syncthreads();
+    return before;
+}
+
+__global__ __launch_bounds__(kThreads) void sort_scatter_kernel(EmbedArgs a, SortPass s) {
+    extern __shared__ uint32_t s_next[];   // 4 waves x digits: first the numbers, then the next place of a digit
+    __shared__ uint32_t s_wave[kThreads / 64u];
+    const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6, digits = 1u << s.bits;
+    const uint32_t first = blockIdx.x * s.tile, end = a.count - first < s.tile ? a.count : first + s.tile;
+    const uint32_t from = first + wave * (s.tile / 4u), to = end < from + s.tile / 4u ? end : from + s.tile / 4u;
+    uint32_t* mine = s_next + wave * digits;
+    for (uint32_t d = t; d < 4u * digits; d += kThreads) s_next[d] = 0u;
+    __syncthreads();
+    // every wave has a run of the tile, of which it counts the digits ...
+    for (uint32_t i0 = from; i0 < to; i0 += 64u) {
+        const uint32_t i = i0 + lane;
+        const bool in = i < to;
+        const uint32_t digit = in ? ((s.keys ? s.keys[i] : key_at(a, i)) >> s.shift) & (digits - 1u) : 0u;
+        const uint64_t same = same_digit(digit, s.bits, __ballot(in));
+        if (in && (same & ((1ull << lane) - 1ull)) == 0ull) mine[digit] += (uint32_t)__popcll(same);
+        wave_fence();
+    }
+    __syncthreads();
+    // ... from which follows where its keys go: behind all smaller digits, and behind its own of earlier tiles and waves
+    const uint32_t each = (digits + kThreads - 1u) / kThreads;
+    uint32_t total = 0u;
+    for (uint32_t e = 0; e < each; ++e) {
+        const uint32_t d = t * each + e;
+        if (d >= digits) break;
+        for (uint32_t tile = 0; tile < gridDim.x; ++tile) total += s.counts[(uint64_t)tile * digits + d];
+    }
+    uint32_t at = sum_before(total, s_wave);
+    for (uint32_t e = 0; e < each; ++e) {
+        const uint32_t d = t * each + e;
+        if (d >= digits) break;
+        uint32_t here = at;
+        for (uint32_t tile = 0; tile < gridDim.x; ++tile) {
+            const uint32_t n = s.counts[(uint64_t)tile * digits + d];
+            at += n;
+            here += tile < blockIdx.x ? n : 0u;
+        }
+        for (uint32_t w = 0; w < 4u; ++w) {
+            const uint32_t n = s_next[w * digits + d];
+            s_next[w * digits + d] = here;
+            here += n;
         }
     }
+    __syncthreads();
+    for (uint32_t i0 = from; i0 < to; i0 += 64u) {
+        const uint32_t i = i0 + lane;
+        const bool in = i < to;
+        const uint32_t key = in ? (s.keys ? s.keys[i] : key_at(a, i)) : 0u, digit = (key >> s.shift) & (digits - 1u);
+        const uint64_t same = same_digit(digit, s.bits, __ballot(in)), below = same & ((1ull << lane) - 1ull);
+        const uint32_t next = mine[digit];
+        wave_fence();
+        if (in) {
+            const uint32_t place = next + (uint32_t)__popcll(below);
+            s.keys_out[place] = key;
+            s.places_out[place] = s.keys ? s.places[i] : i;
+            if (below == 0ull) mine[digit] = next + (uint32_t)__popcll(same);
+        }
+        wave_fence();
+    }
 }
 
-uint32_t grid_for(uint64_t blocks) { return (uint32_t)(blocks < (1u << 20) ? blocks : (1u << 20)); }
+// Up to kFew tokens: the whole sort in one workgroup, in LDS, 8 bits at a time.
+constexpr uint32_t kFew = 4096, kFewThreads = 1024;
+__global__ __launch_bounds__(kFewThreads) void sort_few_kernel(EmbedArgs a, uint32_t* keys_out, uint32_t* places_out, uint32_t key_bits) {
+    constexpr uint32_t kWaves = kFewThreads / 64u;
+    __shared__ uint32_t s_key[2][kFew], s_place[2][kFew], s_next[kWaves][256], s_wave[kWaves];
+    const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6;
+    // a wave has a run of whole groups of 64
+    const uint32_t groups = (a.count + 63u) / 64u, share = (groups + kWaves - 1u) / kWaves * 64u;
+    const uint32_t from = wave * share < a.count ? wave * share : a.count, to = a.count - from < share ? a.count : from + share;
+    for (uint32_t i = t; i < a.count; i += kFewThreads) {
+        s_key[0][i] = key_at(a, i);
+        s_place[0][i] = i;
+    }
+    uint32_t b = 0;
+    for (uint32_t shift = 0; shift < key_bits; shift += 8u, b ^= 1u) {
+        for (uint32_t d = t; d < kWaves * 256u; d += kFewThreads) s_next[0][d] = 0u;
+        __syncthreads();
+        for (uint32_t i0 = from; i0 < to; i0 += 64u) {
+            const uint32_t i = i0 + lane;
+            const bool in = i < to;
+            const uint32_t digit = in ? (s_key[b][i] >> shift) & 255u : 0u;
+            const uint64_t same = same_digit(digit, 8u, __ballot(in));
+            if (in && (same & ((1ull << lane) - 1ull)) == 0ull) s_next[wave][digit] += (uint32_t)__popcll(same);
+            wave_fence();
+        }
+        __syncthreads();
+        uint32_t total = 0u;
+        if (t < 256u)
+            for (uint32_t w = 0; w < kWaves; ++w) total += s_next[w][t];
+        uint32_t at = sum_before(total, s_wave);
+        if (t < 256u)
+            for (uint32_t w = 0; w < kWaves; ++w) {
+                const uint32_t n = s_next[w][t];
+                s_next[w][t] = at;
+                at += n;
+            }
+        __syncthreads();
+        for (uint32_t i0 = from; i0 < to; i0 += 64u) {
+            const uint32_t i = i0 + lane;
+            const bool in = i < to;
+            const uint32_t key = in ? s_key[b][i] : 0u, digit = (key >> shift) & 255u;
+            const uint64_t same = same_digit(digit, 8u, __ballot(in)), below = same & ((1ull << lane) - 1ull);
+            const uint32_t next = s_next[wave][digit];
+            wave_fence();
+            if (in) {
+                const uint32_t place = next + (uint32_t)__popcll(below);
+                s_key[b ^ 1u][place] = key;
+                s_place[b ^ 1u][place] = s_place[b][i];
+                if (below == 0ull) s_next[wave][digit] = next + (uint32_t)__popcll(same);
+            }
+            wave_fence();
+        }
+        __syncthreads();
+    }
+    for (uint32_t i = t; i < a.count; i += kFewThreads) {
+        keys_out[i] = s_key[b][i];
+        places_out[i] = s_place[b][i];
+    }
+}
+
+// ---------------------------------------------------------------- sums of the runs
+struct SumArgs {
+    const uint32_t* keys;     // sorted
+    const uint32_t* places;
+    float* parts;             // 2 x pieces x pitch: what a piece has of a run begun before it, and of one that goes on behind it
+    uint64_t pitch;           // dim rounded up to a multiple of 8
+    uint32_t piece, pieces;   // entries of a piece, and how many
+    uint32_t lanes;           // of a group: a power of two
+    uint32_t slices;          // groups side by side on a row
+    uint32_t sum_groups;      // workgroups that sum; the others write zeros
+};
+
+// First entry whose key is at least `key`.
+__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t count, uint32_t key) {
+    uint32_t lo = 0, hi = count;
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2u;
+        if (keys[mid] < key) lo = mid + 1u;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <bool OUT>
+__device__ __forceinline__ void finish_row(const EmbedArgs& a, uint32_t key, uint32_t d, uint32_t valid, const float (&sum)[8]) {
+    float v[8];
+    const uint64_t at = (uint64_t)key * a.ld_out + d;
+    if (a.accumulate) load_row<OUT>(a.out, at, valid, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = a.accumulate ? v[e] + sum[e] * a.scale : sum[e] * a.scale;
+    store_row<OUT>(a.out, at, valid, v);
+}
+
+constexpr uint32_t kZeroRows = 32;   // rows of the table that a workgroup looks after
+
+template <bool IN, bool OUT>
+__global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
+    if (blockIdx.x >= s.sum_groups) {
+        // Rows whose token does not occur.
+        __shared__ uint32_t s_present;
+        const uint32_t chunks = (a.dim + 7u) / 8u, t = threadIdx.x;
+        const float zero[8] = {};
+        for (uint64_t v0 = (uint64_t)(blockIdx.x - s.sum_groups) * kZeroRows; v0 < a.vocab; v0 += (uint64_t)(gridDim.x - s.sum_groups) * kZeroRows) {
+            if (t < 64u) {
+                bool present = true;
+                if (t < kZeroRows && v0 + t < a.vocab) {
+                    const uint32_t v = (uint32_t)v0 + t, i = lower_bound(s.keys, a.count, v);
+                    present = i < a.count && s.keys[i] == v;
+                }
+                const uint64_t mask = __ballot(present);
+                if (t == 0u) s_present = (uint32_t)mask;
+            }
+            __syncthreads();
+            const uint32_t absent = ~s_present;
+            for (uint32_t r = 0; r < kZeroRows; ++r) {
+                if (!((absent >> r) & 1u)) continue;
+                for (uint32_t c = t; c < chunks; c += kThreads)
+                    store_row<OUT>(a.out, (v0 + r) * a.ld_out + 8u * c, a.dim - 8u * c, zero);
+            }
+            __syncthreads();
+        }
+        return;
+    }
+    const uint64_t group = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / s.lanes;
+    const uint32_t p = (uint32_t)(group / s.slices), slice = (uint32_t)(group % s.slices);
+    const uint32_t d = (slice * s.lanes + threadIdx.x % s.lanes) * 8u;
+    if (p >= s.pieces || d >= a.dim) return;
+    const uint32_t valid = a.dim - d, begin = p * s.piece, end = a.count - begin < s.piece ? a.count : begin + s.piece;
+    uint32_t key = s.keys[begin];
+    bool open = begin != 0u && s.keys[begin - 1u] == key;   // the run has begun before the piece
+    float sum[8] = {};
+    float* part = s.parts + (uint64_t)p * s.pitch + d;
+    auto keep = [&](float* to) { Row8<false>::store(to, sum); };
+    constexpr uint32_t kAhead = 4;
+    for (uint32_t i = begin; i < end; i += kAhead) {
+        uint32_t k[kAhead];
+        float v[kAhead][8];
+#pragma unroll
+        for (uint32_t q = 0; q < kAhead; ++q) {
+            const uint32_t j = i + q < end ? i + q : end - 1u;
+            k[q] = s.keys[j];
+            if (k[q] < a.vocab) load_row<IN>(a.in, (uint64_t)s.places[j] * a.ld_in + d, valid, v[q]);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kAhead; ++q) {
+            if (i + q >= end) continue;
+            if (k[q] != key) {
+                if (open) keep(part);
+                else finish_row<OUT>(a, key, d, valid, sum);
+                key = k[q];
+                open = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+            }
+            if (key < a.vocab)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += v[q][e];
+        }
+        if (key >= a.vocab) return;   // (nothing but such follows)
+    }
+    if (open) keep(part);
+    else if (end < a.count && s.keys[end] == key) keep(part + (uint64_t)s.pieces * s.pitch);
+    else finish_row<OUT>(a, key, d, valid, sum);
+}
+
+// Runs that cross a border: the piece in which one begins adds what the others have of it, in their order.
+template <bool OUT>
+__global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, SumArgs s) {
+    const uint64_t group = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / s.lanes;
+    const uint32_t p = (uint32_t)(group / s.slices), slice = (uint32_t)(group % s.slices);
+    const uint32_t d = (slice * s.lanes + threadIdx.x % s.lanes) * 8u;
+    if (p + 1u >= s.pieces || d >= a.dim) return;
+    const uint32_t begin = p * s.piece, end = begin + s.piece, key = s.keys[end - 1u];
+    if (key >= a.vocab || s.keys[end] != key) return;                                        // nothing goes on
+    if (s.keys[begin] == key && begin != 0u && s.keys[begin - 1u] == key) return;            // it has begun before
+    const uint32_t last = (lower_bound(s.keys, a.count, key + 1u) - 1u) / s.piece;
+    float sum[8];
+    load_row<false>(s.parts, ((uint64_t)s.pieces + p) * s.pitch + d, 8u, sum);
+    for (uint32_t q = p + 1u; q <= last; q += 8u) {
+        float v[8][8];
+#pragma unroll
+        for (uint32_t r = 0; r < 8u; ++r)
+            load_row<false>(s.parts, (uint64_t)(q + r <= last ? q + r : last) * s.pitch + d, 8u, v[r]);
+#pragma unroll
+        for (uint32_t r = 0; r < 8u; ++r)
+            if (q + r <= last)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += v[r][e];
+    }
+    finish_row<OUT>(a, key, d, a.dim - d, sum);
+}
+
+// No tokens at all: zeros.
+template <bool OUT>
+__global__ __launch_bounds__(kThreads) void embed_zero_kernel(EmbedArgs a, uint32_t pieces) {
+    const uint64_t total = (uint64_t)a.vocab * pieces, step = (uint64_t)gridDim.x * kThreads;
+    const float zero[8] = {};
+    for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
+        const uint32_t d = (uint32_t)(i % pieces) * 8u;
+        store_row<OUT>(a.out, i / pieces * a.ld_out + d, a.dim - d, zero);
+    }
+}
+
+uint32_t grid_for(uint64_t threads) {
+    const uint64_t blocks = (threads + kThreads - 1u) / kThreads;
+    return (uint32_t)(blocks < (1u << 20) ? blocks : (1u << 20));
+}
+
+// How the gradient's tokens are sorted and cut, by the sizes alone.
+struct EmbedPlan {
+    uint32_t key_bits, passes, bits, tile, tiles;   // of the sort
+    uint32_t piece, pieces, lanes, slices;          // of the sums
+    uint64_t pitch;
+    uint64_t list, counts, parts;                   // words: of one sorted array, of the counts, of the parts
+};
+EmbedPlan plan_for(uint64_t count, uint64_t vocab, uint64_t dim) {
+    EmbedPlan p{};
+    while (vocab >> p.key_bits) ++p.key_bits;       // keys are 0 .. vocab
+    p.passes = (p.key_bits + 10u) / 11u;
+    p.bits = (p.key_bits + p.passes - 1u) / p.passes;
+    // a tile for each workgroup, 1024 keys or, from 2^18 tokens on, as many as make 256 tiles
+    const uint64_t share = (count + 255u) / 256u;
+    p.tile = (uint32_t)(share < 1024u ? 1024u : (share + 255u) / 256u * 256u);
+    p.tiles = (uint32_t)((count + p.tile - 1u) / p.tile);
+    // pieces of 16 entries or, from 2^15 tokens on, as many as make 2048 pieces: a run that crosses all of them is added by one group
+    const uint64_t entries = (count + 2047u) / 2048u;
+    p.piece = (uint32_t)(entries < 16u ? 16u : entries);
+    p.pieces = (uint32_t)((count + p.piece - 1u) / p.piece);
+    const uint64_t chunks = (dim + 7u) / 8u;
+    p.lanes = 1u;
+    while (p.lanes < 64u && p.lanes < chunks) p.lanes *= 2u;
+    p.slices = (uint32_t)((chunks + p.lanes - 1u) / p.lanes);
+    p.pitch = 8u * chunks;
+    p.list = (count + 3u) / 4u * 4u;
+    p.counts = count > kFew ? (uint64_t)p.tiles << p.bits : 0u;
+    p.parts = 2u * p.pieces * p.pitch;
+    return p;
+}
 
 }  // namespace
 
 hipError_t launch_embed_forward(const EmbedArgs& a, hipStream_t stream) {
-    embed_forward_kernel<<<grid_for(a.count), kThreads, 0, stream>>>(a);
+    const uint32_t pieces = (a.dim + 7u) / 8u, grid = grid_for((uint64_t)a.count * pieces);
+    auto go = [&](auto I, auto O) {
+        embed_forward_kernel<decltype(I)::value, decltype(O)::value><<<grid, kThreads, 0, stream>>>(a, pieces);
+    };
+    auto out = [&](auto I) { a.out_bf16 ? go(I, std::true_type{}) : go(I, std::false_type{}); };
+    a.in_bf16 ? out(std::true_type{}) : out(std::false_type{});
     return hipGetLastError();
 }
 
-uint64_t embed_backward_workspace_bytes(uint64_t, uint64_t, uint64_t) { return 0; }
+uint64_t embed_backward_workspace_bytes(uint64_t count, uint64_t vocab, uint64_t dim) {
+    if (count == 0 || vocab == 0 || dim == 0) return 0;
+    const EmbedPlan p = plan_for(count, vocab, dim);
+    return 4u * (4u * p.list + (p.counts + 3u) / 4u * 4u + p.parts);
+}
 
 hipError_t launch_embed_backward(const EmbedArgs& a, hipStream_t stream) {
-    embed_backward_simple_kernel<<<grid_for(a.vocab), kThreads, 0, stream>>>(a);
+    if (a.count == 0u) {
+        const uint32_t pieces = (a.dim + 7u) / 8u, grid = grid_for((uint64_t)a.vocab * pieces);
+        if (a.out_bf16) embed_zero_kernel<true><<<grid, kThreads, 0, stream>>>(a, pieces);
+        else embed_zero_kernel<false><<<grid, kThreads, 0, stream>>>(a, pieces);
+        return hipGetLastError();
+    }
+    const EmbedPlan p = plan_for(a.count, a.vocab, a.dim);
+    uint32_t* list[4];
+    for (int i = 0; i < 4; ++i) list[i] = a.workspace + i * p.list;
+    uint32_t* counts = a.workspace + 4u * p.list;
+    SumArgs s{};
+    s.parts = reinterpret_cast<float*>(counts + (p.counts + 3u) / 4u * 4u);
+    s.pitch = p.pitch;
+    s.piece = p.piece;
+    s.pieces = p.pieces;
+    s.lanes = p.lanes;
+    s.slices = p.slices;
+    if (a.count <= kFew) {
+        sort_few_kernel<<<1, kFewThreads, 0, stream>>>(a, list[0], list[1], p.key_bits);
+        s.keys = list[0];
+        s.places = list[1];
+    } else {
+        for (uint32_t pass = 0; pass < p.passes; ++pass) {
+            SortPass sort{};
+            sort.keys = pass ? list[2u * ((pass - 1u) & 1u)] : nullptr;
+            sort.places = pass ? list[2u * ((pass - 1u) & 1u) + 1u] : nullptr;
+            sort.keys_out = list[2u * (pass & 1u)];
+            sort.places_out = list[2u * (pass & 1u) + 1u];
+            sort.counts = counts;
+            sort.tile = p.tile;
+            sort.shift = pass * p.bits;
+            sort.bits = p.bits;
+            sort_count_kernel<<<p.tiles, kThreads, 4u << p.bits, stream>>>(a, sort);
+            sort_scatter_kernel<<<p.tiles, kThreads, 16u << p.bits, stream>>>(a, sort);
+            s.keys = sort.keys_out;
+            s.places = sort.places_out;
+        }
+    }
+    const uint64_t groups = (uint64_t)p.pieces * p.slices * p.lanes;
+    s.sum_groups = (uint32_t)((groups + kThreads - 1u) / kThreads);
+    const uint32_t zero_rows = (a.vocab + kZeroRows - 1u) / kZeroRows, zero_groups = a.accumulate ? 0u : zero_rows < (1u << 20) ? zero_rows : 1u << 20;
+    auto out = [&](auto O) {
+        constexpr bool OUT = decltype(O)::value;
+        if (a.in_bf16) embed_sum_kernel<true, OUT><<<s.sum_groups + zero_groups, kThreads, 0, stream>>>(a, s);
+        else embed_sum_kernel<false, OUT><<<s.sum_groups + zero_groups, kThreads, 0, stream>>>(a, s);
+        if (p.pieces > 1u) embed_join_kernel<OUT><<<s.sum_groups, kThreads, 0, stream>>>(a, s);
+    };
+    a.out_bf16 ? out(std::true_type{}) : out(std::false_type{});
     return hipGetLastError();
 }
 
