@@ -293,8 +293,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
     if (blockIdx.x >= s.sum_groups) {
         // Rows whose token does not occur.
         __shared__ uint32_t s_present;
-        const uint32_t chunks = (a.dim + 7u) / 8u, t = threadIdx.x;
-        const float zero[8] = {};
+        constexpr uint32_t kEach = OUT ? 8u : 4u;   // values in 16 bytes
+        const uint32_t t = threadIdx.x;
         for (uint64_t v0 = (uint64_t)(blockIdx.x - s.sum_groups) * kZeroRows; v0 < a.vocab; v0 += (uint64_t)(gridDim.x - s.sum_groups) * kZeroRows) {
             if (t < 64u) {
                 bool present = true;
@@ -309,8 +309,14 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
             const uint32_t absent = ~s_present;
             for (uint32_t r = 0; r < kZeroRows; ++r) {
                 if (!((absent >> r) & 1u)) continue;
-                for (uint32_t c = t; c < chunks; c += kThreads)
-                    store_row<OUT>(a.out, (v0 + r) * a.ld_out + 8u * c, a.dim - 8u * c, zero);
+                uint8_t* row = static_cast<uint8_t*>(a.out) + (v0 + r) * a.ld_out * (OUT ? 2u : 4u);
+                for (uint32_t c = kEach * t; c < a.dim; c += kEach * kThreads) {
+                    if (c + kEach <= a.dim) {
+                        store16(row + c * (OUT ? 2u : 4u), make_uint4(0u, 0u, 0u, 0u));
+                        continue;
+                    }
+                    for (uint32_t d = c; d < a.dim; ++d) store1<OUT>(row + d * (OUT ? 2u : 4u), 0.0f, false);
+                }
             }
             __syncthreads();
         }
@@ -413,9 +419,10 @@ EmbedPlan plan_for(uint64_t count, uint64_t vocab, uint64_t dim) {
     while (vocab >> p.key_bits) ++p.key_bits;       // keys are 0 .. vocab
     p.passes = (p.key_bits + 10u) / 11u;
     p.bits = (p.key_bits + p.passes - 1u) / p.passes;
-    // a tile for each workgroup, 1024 keys or, from 2^18 tokens on, as many as make 256 tiles
+    // a tile for each workgroup, 256 keys (one look at 64 keys for each of its waves) or, from 2^16 tokens on, as many as make 256
+    // tiles
     const uint64_t share = (count + 255u) / 256u;
-    p.tile = (uint32_t)(share < 1024u ? 1024u : (share + 255u) / 256u * 256u);
+    p.tile = (uint32_t)((share + 255u) / 256u * 256u);
     p.tiles = (uint32_t)((count + p.tile - 1u) / p.tile);
     // pieces of 16 entries or, from 2^15 tokens on, as many as make 2048 pieces: a run that crosses all of them is added by one group
     const uint64_t entries = (count + 2047u) / 2048u;

@@ -174,12 +174,22 @@ __device__ __forceinline__ void store1(void* c, float v, bool accumulate) {
 
 // `left` (at least 1) of 4 neighbouring values of a row.
 template <bool BF16>
-__device__ __forceinline__ void store4(void* c, const f32x4& v, uint32_t left, bool accumulate) {
-    if (left >= 4u && !accumulate) {
+__device__ __forceinline__ void store4(void* c, f32x4 v, uint32_t left, bool accumulate) {
+    typedef uint32_t words2_any __attribute__((ext_vector_type(2), aligned(2)));
+    if (left >= 4u) {
         if (BF16) {
-            typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-            *static_cast<u32x2_any*>(c) = u32x2_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+            if (accumulate) {
+                const words2_any o = *static_cast<const words2_any*>(c);
+                v[0] += bf16_low(o[0]); v[1] += bf16_high(o[0]);
+                v[2] += bf16_low(o[1]); v[3] += bf16_high(o[1]);
+            }
+            *static_cast<words2_any*>(c) = words2_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
         } else {
+            if (accumulate) {
+                const uint4 o = load16(c);
+                v[0] += __uint_as_float(o.x); v[1] += __uint_as_float(o.y);
+                v[2] += __uint_as_float(o.z); v[3] += __uint_as_float(o.w);
+            }
             store16(c, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
         }
         return;

@@ -237,43 +237,68 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     if (k + 3u < steps) step(std::integral_constant<uint32_t, 3>{}, k + 3u);
     __builtin_amdgcn_s_waitcnt(0x0F70);   // (what was fetched behind the last step)
 
-    // 32 rows' sums at a time out of the matrix unit's registers, 8 neighbouring ones a lane.  One of several parts keeps its
-    // sums as they are, in rows with room up to a multiple of 8.
-    constexpr bool BF16 = !EXACT;
-    constexpr uint32_t kSize = BF16 ? 2u : 4u;
-    const bool part = a.share < blocks, add = a.accumulate && !part;
-    const uint64_t pitch = fp8_part_pitch(a.N);
-    float* sums = a.workspace + blockIdx.y * a.M * pitch;
-    const uint32_t n = n0 + wn * 32u * NF + 8u * h;
+    // 32 rows of a wave at a time by way of LDS, so that a row leaves in whole lines: stored as the matrix unit holds them, two
+    // lanes to a row, the writes of all workgroups took the caches ten times as long.  Pieces of 16 bytes are kept at places
+    // exchanged by row, as above.  One of several parts keeps its sums in fp32, in rows with room up to a multiple of 8.
+    __builtin_amdgcn_s_barrier();   // (nothing is on its way to LDS any more)
+    auto emit = [&](auto wide, auto half, void* out, uint64_t pitch, uint32_t columns, bool add) {   // sums kept in fp32; bf16 results
+        constexpr bool kWide = decltype(wide)::value, kHalf16 = decltype(half)::value;
+        constexpr uint32_t kPieces = (kWide ? 8u : 4u) * NF, kEach = kWide ? 4u : 8u;   // of a row, and values of one
+        static_assert(32u * kPieces * 16u <= kUnit, "a strip fits a unit");
+        uint8_t* strip = wave == 0u ? s0 : wave == 1u ? s1 : wave == 2u ? s2 : s3;
+        auto place = [&](uint32_t r, uint32_t piece) {
+            return reinterpret_cast<uint4*>(strip + (r * kPieces + (piece ^ (kPieces >= 16u ? r & 15u : (r >> 1) & 7u))) * 16u);
+        };
+        const uint32_t nw = n0 + wn * 32u * NF;
 #pragma unroll
-    for (uint32_t i = 0; i < MF; ++i) {
-        const uint32_t m = m0 + wm * 32u * MF + i * 32u + x;
-        __builtin_amdgcn_sched_barrier(0);
-        if (m >= a.M) continue;
-        uint8_t* at = static_cast<uint8_t*>(a.c) + ((uint64_t)m * a.ldc + n) * kSize;
-        Row8<BF16> old[2 * NF] = {};
-        if (add) {
+        for (uint32_t i = 0; i < MF; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (uint32_t j = 0; j < 2u * NF; ++j)
-                if (n + 16u * j + 8u <= a.N) old[j].load(at + j * 16u * kSize);
-        }
+            for (uint32_t j = 0; j < 2u * NF; ++j) {
+                float v[8];
 #pragma unroll
-        for (uint32_t j = 0; j < 2u * NF; ++j) {
-            const uint32_t nj = n + 16u * j;
-            float v[8];
-#pragma unroll
-            for (uint32_t e = 0; e < 8u; ++e) v[e] = acc[i][j >> 1][8u * (j & 1u) + e];
-            if (part) {
-                if (nj < a.N) Row8<false>::store(sums + m * pitch + nj, v);
-            } else if (nj + 8u <= a.N) {
-                if (add) old[j].add_to(v);
-                Row8<BF16>::store(at + j * 16u * kSize, v);
-            } else {
-#pragma unroll
-                for (uint32_t e = 0; e < 7u; ++e)
-                    if (nj + e < a.N) store1<BF16>(at + (j * 16u + e) * kSize, v[e], add);
+                for (uint32_t e = 0; e < 8u; ++e) v[e] = acc[i][j >> 1][8u * (j & 1u) + e];
+                const uint32_t g = 2u * j + h;   // 8 columns
+                if (kWide) {
+                    *place(x, 2u * g) = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                    *place(x, 2u * g + 1u) = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+                } else {
+                    *place(x, g) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+                }
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (uint32_t it = 0; it < kPieces / 2u; ++it) {
+                const uint32_t r = it * (64u / kPieces) + lane / kPieces, piece = lane % kPieces;
+                const uint32_t m = m0 + wm * 32u * MF + i * 32u + r, n = nw + piece * kEach;
+                const uint4 w = *place(r, piece);
+                if (m >= a.M || n >= columns) continue;
+                uint8_t* at = static_cast<uint8_t*>(out) + (m * pitch + n) * (kHalf16 ? 2u : 4u);
+                if (kWide) {
+                    store4<kHalf16>(at, f32x4{__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)}, columns - n, add);
+                } else if (n + 8u <= columns) {
+                    store16(at, w);
+                } else {
+                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (uint32_t e = 0; e < 7u; ++e)
+                        if (n + e < columns) reinterpret_cast<uint16_t*>(at)[e] = (uint16_t)(words[e >> 1] >> (e & 1u ? 16 : 0));
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
         }
+    };
+    if (a.share < blocks) {
+        const uint64_t pitch = fp8_part_pitch(a.N);
+        emit(std::true_type{}, std::false_type{}, a.workspace + blockIdx.y * a.M * pitch, pitch, (uint32_t)pitch, false);
+    } else if constexpr (EXACT) {
+        emit(std::true_type{}, std::false_type{}, a.c, a.ldc, a.N, a.accumulate);
+    } else if (a.accumulate) {   // (the old value is added before the only rounding)
+        emit(std::true_type{}, std::true_type{}, a.c, a.ldc, a.N, true);
+    } else {
+        emit(std::false_type{}, std::true_type{}, a.c, a.ldc, a.N, false);
     }
 }
 

@@ -29,40 +29,88 @@ __device__ __forceinline__ uint32_t row16_umax(uint32_t x) {
     return x;
 }
 
-// 8 neighbouring values, of which `valid` exist.
+// 8 neighbouring values, of which `valid` exist, as they lie in memory.
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* x, uint64_t at, uint32_t valid, float (&v)[8]) {
-    if (valid >= 8u) {
-        if (BF16) {
-            const uint4 q = load16(static_cast<const uint16_t*>(x) + at);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+struct Eight {
+    static constexpr int kWords = BF16 ? 4 : 8;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const void* x, uint64_t at, uint32_t valid) {
+        if (valid >= 8u) {
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                v[2 * d] = bf16_low(w[d]);
-                v[2 * d + 1] = bf16_high(w[d]);
+            for (int d = 0; d < kWords / 4; ++d) {
+                const uint4 q = load16(static_cast<const uint8_t*>(x) + at * (BF16 ? 2u : 4u) + 16 * d);
+                w[4 * d] = q.x;
+                w[4 * d + 1] = q.y;
+                w[4 * d + 2] = q.z;
+                w[4 * d + 3] = q.w;
             }
-        } else {
+            return;
+        }
 #pragma unroll
-            for (int d = 0; d < 2; ++d) {
-                const uint4 q = load16(static_cast<const float*>(x) + at + 4 * d);
-                v[4 * d] = __uint_as_float(q.x);
-                v[4 * d + 1] = __uint_as_float(q.y);
-                v[4 * d + 2] = __uint_as_float(q.z);
-                v[4 * d + 3] = __uint_as_float(q.w);
+        for (uint32_t e = 0; e < 8u; ++e) {
+            if (BF16) {
+                const uint32_t v = e < valid ? static_cast<const uint16_t*>(x)[at + e] : 0u;
+                if (e & 1u) w[e >> 1] |= v << 16;
+                else w[e >> 1] = v;
+            } else {
+                w[BF16 ? 0 : e] = e < valid ? static_cast<const uint32_t*>(x)[at + e] : 0u;
             }
         }
-        return;
     }
+    // the larger magnitude, word by word (bf16: of both halves)
+    static __device__ __forceinline__ uint32_t larger(uint32_t top, uint32_t word) {
+        if (BF16) return max_u16x2(top, word & 0x7FFF7FFFu);
+        const uint32_t m = word & 0x7FFFFFFFu;
+        return m > top ? m : top;
+    }
+    // of both halves, as fp32 bits
+    static __device__ __forceinline__ uint32_t whole(uint32_t top) {
+        if (!BF16) return top;
+        const uint32_t lo = top << 16, hi = top & 0xFFFF0000u;
+        return lo > hi ? lo : hi;
+    }
+    __device__ __forceinline__ uint32_t amax() const {
+        uint32_t m = 0u;
 #pragma unroll
-    for (uint32_t e = 0; e < 8u; ++e) {
-        float f = 0.0f;
-        if (e < valid)
-            f = BF16 ? bf16_low(static_cast<const uint16_t*>(x)[at + e]) : static_cast<const float*>(x)[at + e];
-        v[e] = f;
+        for (int d = 0; d < kWords; ++d) m = larger(m, w[d]);
+        return whole(m);
     }
-}
+    template <bool E5M2>
+    __device__ __forceinline__ uint2 codes(uint32_t e) const {
+        const float scale = fp8_scale(e);
+        uint2 c;
+        if constexpr (BF16) {
+            c.x = fp8_codes_bf16<E5M2>(w[0], w[1], scale);
+            c.y = fp8_codes_bf16<E5M2>(w[2], w[3], scale);
+        } else {
+            c.x = fp8_codes<E5M2>(value(0), value(1), value(2), value(3), scale);
+            c.y = fp8_codes<E5M2>(value(4), value(5), value(6), value(7), scale);
+        }
+        if (e == 255u) c.x = c.y = 0x7F7F7F7Fu;
+        return c;
+    }
+    __device__ __forceinline__ float value(int e) const { return __uint_as_float(w[e]); }   // (fp32 only)
+};
 
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+// Codes of column j of 8 rows.
+template <bool BF16, bool E5M2>
+__device__ __forceinline__ uint2 column_codes(const Eight<BF16> (&v)[8], int j, uint32_t e) {
+    const float scale = fp8_scale(e);
+    uint2 c;
+    if constexpr (BF16) {
+        const uint32_t halves = j & 1 ? 0x07060302u : 0x05040100u;   // of the second word and the first
+        uint32_t pair[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) pair[p] = __builtin_amdgcn_perm(v[2 * p + 1].w[j >> 1], v[2 * p].w[j >> 1], halves);
+        c.x = fp8_codes_bf16<E5M2>(pair[0], pair[1], scale);
+        c.y = fp8_codes_bf16<E5M2>(pair[2], pair[3], scale);
+    } else {
+        c.x = fp8_codes<E5M2>(v[0].value(j), v[1].value(j), v[2].value(j), v[3].value(j), scale);
+        c.y = fp8_codes<E5M2>(v[4].value(j), v[5].value(j), v[6].value(j), v[7].value(j), scale);
+    }
+    if (e == 255u) c.x = c.y = 0x7F7F7F7Fu;
+    return c;
+}
 
 // The byte of block j in its scale word, and zeros behind the last block.
 __device__ __forceinline__ void store_scale(uint32_t* scales, uint32_t rows, uint32_t r, uint32_t j, uint32_t blocks, uint32_t e) {
@@ -74,7 +122,8 @@ __device__ __forceinline__ void store_scale(uint32_t* scales, uint32_t rows, uin
 
 template <bool BF16, bool E5M2, bool TILE>
 __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs a, uint32_t tiles_c, uint64_t tiles) {
-    __shared__ uint32_t s_max[16][kTile];
+    constexpr int kWords = Eight<BF16>::kWords;
+    __shared__ uint32_t s_max[16][kTile];   // (bf16: two columns to a word)
     __shared__ uint2 s_code[kTile][16];
     __shared__ uint32_t s_row[kTile], s_col[kTile];
     const uint32_t t = threadIdx.x, cg = t & 15u, rg = t >> 4;
@@ -84,25 +133,15 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs 
     for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const uint32_t tr = (uint32_t)(tile / tiles_c), tc = (uint32_t)(tile % tiles_c);
         const uint32_t r0 = tr * kTile + rg * 8u, c0 = tc * kTile + cg * 8u;
-        float v[8][8];
+        Eight<BF16> v[8];
 #pragma unroll
         for (uint32_t p = 0; p < 8u; ++p) {
             const uint32_t r = r0 + p, valid = r < a.rows && c0 < a.cols ? a.cols - c0 : 0u;
-            load8<BF16>(a.x, (uint64_t)r * a.ld + c0, valid, v[p]);
+            v[p].load(a.x, (uint64_t)r * a.ld + c0, valid);
         }
-        uint32_t rm[8], cm[8];
+        uint32_t rm[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) rm[i] = cm[i] = 0u;
-#pragma unroll
-        for (int p = 0; p < 8; ++p)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t m = magnitude(v[p][j]);
-                rm[p] = m > rm[p] ? m : rm[p];
-                cm[j] = m > cm[j] ? m : cm[j];
-            }
-#pragma unroll
-        for (int p = 0; p < 8; ++p) rm[p] = row16_umax(rm[p]);
+        for (int p = 0; p < 8; ++p) rm[p] = row16_umax(v[p].amax());
         if (TILE) {
             uint32_t m = 0u;
 #pragma unroll
@@ -122,7 +161,12 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs 
             }
             if (a.q_t) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s_max[rg][cg * 8u + j] = cm[j];
+                for (int d = 0; d < kWords; ++d) {
+                    uint32_t m = 0u;
+#pragma unroll
+                    for (int p = 0; p < 8; ++p) m = Eight<BF16>::larger(m, v[p].w[d]);
+                    s_max[rg][cg * kWords + d] = m;
+                }
             }
         }
         __syncthreads();
@@ -130,39 +174,23 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs 
             if (t < kTile) {
                 uint32_t m = 0u;
 #pragma unroll
-                for (int g = 0; g < 16; ++g) {
-                    const uint32_t y = s_max[g][t];
-                    m = y > m ? y : m;
-                }
+                for (int g = 0; g < 16; ++g) m = Eight<BF16>::larger(m, s_max[g][BF16 ? t >> 1 : t]);
+                if (BF16) m = t & 1u ? m & 0xFFFF0000u : m << 16;
                 s_col[t] = fp8_scale_byte<E5M2>(m);
             }
             __syncthreads();
         }
         if (a.q) {
 #pragma unroll
-            for (uint32_t p = 0; p < 8u; ++p) {
-                if (r0 + p >= a.rows) continue;
-                const uint32_t e = fp8_scale_byte<E5M2>(rm[p]);
-                const float scale = fp8_scale(e);
-                uint2 w;
-                w.x = fp8_codes<E5M2>(v[p][0], v[p][1], v[p][2], v[p][3], scale);
-                w.y = fp8_codes<E5M2>(v[p][4], v[p][5], v[p][6], v[p][7], scale);
-                if (e == 255u) w.x = w.y = 0x7F7F7F7Fu;
-                *reinterpret_cast<uint2*>(a.q + (uint64_t)(r0 + p) * q_ld + c0) = w;
-            }
+            for (uint32_t p = 0; p < 8u; ++p)
+                if (r0 + p < a.rows)
+                    *reinterpret_cast<uint2*>(a.q + (uint64_t)(r0 + p) * q_ld + c0) = v[p].template codes<E5M2>(fp8_scale_byte<E5M2>(rm[p]));
             if (t < kTile && tr * kTile + t < a.rows) store_scale(a.scales, a.rows, tr * kTile + t, tc, tiles_c, s_row[t]);
         }
         if (a.q_t) {
 #pragma unroll
-            for (uint32_t j = 0; j < 8u; ++j) {
-                const uint32_t e = s_col[cg * 8u + j];
-                const float scale = fp8_scale(e);
-                uint2 w;
-                w.x = fp8_codes<E5M2>(v[0][j], v[1][j], v[2][j], v[3][j], scale);
-                w.y = fp8_codes<E5M2>(v[4][j], v[5][j], v[6][j], v[7][j], scale);
-                if (e == 255u) w.x = w.y = 0x7F7F7F7Fu;
-                s_code[cg * 8u + j][rg ^ cg] = w;   // (columns 8 apart fall into the same banks)
-            }
+            for (int j = 0; j < 8; ++j)   // (columns 8 apart fall into the same banks)
+                s_code[cg * 8u + j][rg ^ cg] = column_codes<BF16, E5M2>(v, j, s_col[cg * 8u + j]);
             __syncthreads();
 #pragma unroll
             for (uint32_t i = 0; i < 4u; ++i) {
@@ -185,21 +213,10 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_rows_kernel(Fp8Quantize
     const uint64_t q_ld = (uint64_t)blocks * 128u, step = (uint64_t)gridDim.x * (kThreads / 64u);
     for (uint64_t i = (uint64_t)blockIdx.x * (kThreads / 64u) + (threadIdx.x >> 6); i < total; i += step) {
         const uint32_t r = (uint32_t)(i / groups), group = (uint32_t)(i % groups), j = 4u * group + (lane >> 4), c = j * 128u + cg * 8u;
-        float v[8];
-        load8<BF16>(a.x, (uint64_t)r * a.ld + c, c < a.cols ? a.cols - c : 0u, v);
-        uint32_t m = 0u;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t y = magnitude(v[e]);
-            m = y > m ? y : m;
-        }
-        m = row16_umax(m);
-        const uint32_t e = fp8_scale_byte<E5M2>(m);
-        const float scale = fp8_scale(e);
-        uint2 w;
-        w.x = fp8_codes<E5M2>(v[0], v[1], v[2], v[3], scale);
-        w.y = fp8_codes<E5M2>(v[4], v[5], v[6], v[7], scale);
-        if (e == 255u) w.x = w.y = 0x7F7F7F7Fu;
+        Eight<BF16> v;
+        v.load(a.x, (uint64_t)r * a.ld + c, c < a.cols ? a.cols - c : 0u);
+        const uint32_t e = fp8_scale_byte<E5M2>(row16_umax(v.amax()));
+        const uint2 w = v.template codes<E5M2>(e);
         if (j < blocks) *reinterpret_cast<uint2*>(a.q + r * q_ld + c) = w;   // (behind the last block: zeros, and scale 0)
         uint32_t word = e << (8u * (lane >> 4));
         word |= (uint32_t)__shfl_xor((int)word, 16);
@@ -208,42 +225,35 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_rows_kernel(Fp8Quantize
     }
 }
 
-// 16 codes a thread.
+// As many codes a thread as make 16 bytes of values.
 template <bool E5M2, bool BF16OUT>
-__global__ __launch_bounds__(kThreads) void fp8_dequantize_kernel(const uint8_t* q, const uint32_t* scales, uint32_t rows,
-                                                                  uint32_t cols, uint32_t pieces, void* out, uint64_t ld) {
+__global__ __launch_bounds__(kThreads) void fp8_dequantize_kernel(const uint8_t* q, const uint32_t* scales, uint32_t rows, uint32_t cols,
+                                                                  uint32_t pieces, void* out, uint64_t ld) {
+    constexpr uint32_t kEach = BF16OUT ? 8u : 4u;
     const uint64_t total = (uint64_t)rows * pieces, step = (uint64_t)gridDim.x * kThreads;
     const uint64_t q_ld = (cols + 127u) / 128u * 128u;
     for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
-        const uint32_t r = (uint32_t)(i / pieces), c = (uint32_t)(i % pieces) * 16u, j = c >> 7;
-        const uint4 w = *reinterpret_cast<const uint4*>(q + (uint64_t)r * q_ld + c);
+        const uint32_t r = (uint32_t)(i / pieces), c = (uint32_t)(i % pieces) * kEach, j = c >> 7;
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(q + (uint64_t)r * q_ld + c);
         const uint32_t e = (scales[(uint64_t)(j >> 2) * rows + r] >> (8u * (j & 3u))) & 0xFFu;
-        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-        float v[16];
+        float v[kEach];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const auto lo = E5M2 ? __builtin_amdgcn_cvt_pk_f32_bf8((int)word[k], false) : __builtin_amdgcn_cvt_pk_f32_fp8((int)word[k], false);
-            const auto hi = E5M2 ? __builtin_amdgcn_cvt_pk_f32_bf8((int)word[k], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)word[k], true);
+        for (uint32_t k = 0; k < kEach / 4u; ++k) {
+            const auto lo = E5M2 ? __builtin_amdgcn_cvt_pk_f32_bf8((int)w[k], false) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false);
+            const auto hi = E5M2 ? __builtin_amdgcn_cvt_pk_f32_bf8((int)w[k], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
             v[4 * k] = lo[0]; v[4 * k + 1] = lo[1]; v[4 * k + 2] = hi[0]; v[4 * k + 3] = hi[1];
         }
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = e == 255u ? __uint_as_float(0x7FC00000u) : ldexpf(v[k], (int)e - 127);
-        if (c + 16u <= cols) {
-            uint8_t* o = static_cast<uint8_t*>(out) + ((uint64_t)r * ld + c) * (BF16OUT ? 2u : 4u);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float half[8] = {v[8 * k], v[8 * k + 1], v[8 * k + 2], v[8 * k + 3], v[8 * k + 4], v[8 * k + 5], v[8 * k + 6], v[8 * k + 7]};
-                Row8<BF16OUT>::store(o + k * (BF16OUT ? 16 : 32), half);
-            }
+        for (uint32_t k = 0; k < kEach; ++k) v[k] = e == 255u ? __uint_as_float(0x7FC00000u) : ldexpf(v[k], (int)e - 127);
+        uint8_t* o = static_cast<uint8_t*>(out) + ((uint64_t)r * ld + c) * (BF16OUT ? 2u : 4u);
+        if (c + kEach <= cols) {
+            if constexpr (BF16OUT) store16(o, make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])));
+            else store16(o, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
             continue;
         }
 #pragma unroll
-        for (uint32_t k = 0; k < 16u; ++k) {
-            if (c + k >= cols) continue;
-            const uint64_t at = (uint64_t)r * ld + c + k;
-            if (BF16OUT) static_cast<uint16_t*>(out)[at] = bf16_bits(v[k]);
-            else static_cast<float*>(out)[at] = v[k];
-        }
+        for (uint32_t k = 0; k < kEach; ++k)
+            if (c + k < cols) store1<BF16OUT>(o + k * (BF16OUT ? 2u : 4u), v[k], false);
     }
 }
 
@@ -277,7 +287,7 @@ hipError_t launch_fp8_quantize(const Fp8QuantizeArgs& a, bool bf16, bool e5m2, b
 
 hipError_t launch_fp8_dequantize(const uint8_t* q, const uint32_t* scales, bool e5m2, uint32_t rows, uint32_t cols,
                                  bool out_bf16, void* out, uint64_t ld, hipStream_t stream) {
-    const uint32_t pieces = (cols + 15u) / 16u;
+    const uint32_t each = out_bf16 ? 8u : 4u, pieces = (cols + each - 1u) / each;
     const uint32_t grid = grid_for(((uint64_t)rows * pieces + kThreads - 1u) / kThreads);
     auto go = [&](auto E, auto B) {
         fp8_dequantize_kernel<decltype(E)::value, decltype(B)::value>
