@@ -84,6 +84,33 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, uint32_t bits, ui
     return mask;
 }
 
+// Zeros in rows [first, end) of the table, by workgroup `group` of `groups`.
+template <bool OUT>
+__device__ __forceinline__ void zero_rows(const EmbedArgs& a, uint32_t first, uint32_t end, uint32_t group, uint32_t groups) {
+    constexpr uint32_t kEach = OUT ? 8u : 4u, kSize = OUT ? 2u : 4u;   // values in 16 bytes
+    const uint32_t pieces = (a.dim + kEach - 1u) / kEach;
+    const uint64_t total = (uint64_t)(end - first) * pieces, step = (uint64_t)groups * blockDim.x;
+    for (uint64_t i = (uint64_t)group * blockDim.x + threadIdx.x; i < total; i += step) {
+        const uint32_t d = (uint32_t)(i % pieces) * kEach;
+        uint8_t* at = static_cast<uint8_t*>(a.out) + ((first + i / pieces) * a.ld_out + d) * kSize;
+        if (d + kEach <= a.dim) {
+            store16(at, make_uint4(0u, 0u, 0u, 0u));
+            continue;
+        }
+        for (uint32_t e = 0; d + e < a.dim; ++e) store1<OUT>(at + e * kSize, 0.0f, false);
+    }
+}
+// The workgroups of a sorting launch behind the first `sorters`: zeros in their launch's share of the table.
+struct ZeroShare {
+    uint32_t first, end;   // rows
+};
+__device__ __forceinline__ bool zeroes(const EmbedArgs& a, const ZeroShare& z, uint32_t sorters) {
+    if (blockIdx.x < sorters) return false;
+    if (a.out_bf16) zero_rows<true>(a, z.first, z.end, blockIdx.x - sorters, gridDim.x - sorters);
+    else zero_rows<false>(a, z.first, z.end, blockIdx.x - sorters, gridDim.x - sorters);
+    return true;
+}
+
 // Between the accesses of a wave's lanes to what other lanes of the wave have written in LDS.
 __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -99,11 +126,13 @@ struct SortPass {
     uint32_t* places_out;
     uint32_t* counts;        // tiles x digits
     uint32_t tile;           // keys of a tile, a multiple of 256
+    uint32_t tiles;
     uint32_t shift, bits;
 };
 
-__global__ __launch_bounds__(kThreads) void sort_count_kernel(EmbedArgs a, SortPass s) {
+__global__ __launch_bounds__(kThreads) void sort_count_kernel(EmbedArgs a, SortPass s, ZeroShare z) {
     extern __shared__ uint32_t s_count[];
+    if (zeroes(a, z, s.tiles)) return;
     const uint32_t digits = 1u << s.bits, first = blockIdx.x * s.tile, end = a.count - first < s.tile ? a.count : first + s.tile;
     for (uint32_t d = threadIdx.x; d < digits; d += kThreads) s_count[d] = 0u;
     __syncthreads();
@@ -132,9 +161,10 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* s_wave) {
     return before;
 }
 
-__global__ __launch_bounds__(kThreads) void sort_scatter_kernel(EmbedArgs a, SortPass s) {
-    extern __shared__ uint32_t s_next[];   // 4 waves x digits: first the numbers, then the next place of a digit
+__global__ __launch_bounds__(kThreads) void sort_scatter_kernel(EmbedArgs a, SortPass s, ZeroShare z) {
+    extern __shared__ uint32_t s_next[];   // 4 waves x digits: first the numbers, then the next place of a digit; 2 x digits of scratch
     __shared__ uint32_t s_wave[kThreads / 64u];
+    if (zeroes(a, z, s.tiles)) return;
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6, digits = 1u << s.bits;
     const uint32_t first = blockIdx.x * s.tile, end = a.count - first < s.tile ? a.count : first + s.tile;
     const uint32_t from = first + wave * (s.tile / 4u), to = end < from + s.tile / 4u ? end : from + s.tile / 4u;
@@ -152,23 +182,30 @@ __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(EmbedArgs a, Sor
     }
     __syncthreads();
     // ... from which follows where its keys go: behind all smaller digits, and behind its own of earlier tiles and waves
-    const uint32_t each = (digits + kThreads - 1u) / kThreads;
-    uint32_t total = 0u;
-    for (uint32_t e = 0; e < each; ++e) {
-        const uint32_t d = t * each + e;
-        if (d >= digits) break;
-        for (uint32_t tile = 0; tile < gridDim.x; ++tile) total += s.counts[(uint64_t)tile * digits + d];
-    }
-    uint32_t at = sum_before(total, s_wave);
-    for (uint32_t e = 0; e < each; ++e) {
-        const uint32_t d = t * each + e;
-        if (d >= digits) break;
-        uint32_t here = at;
-        for (uint32_t tile = 0; tile < gridDim.x; ++tile) {
-            const uint32_t n = s.counts[(uint64_t)tile * digits + d];
-            at += n;
-            here += tile < blockIdx.x ? n : 0u;
+    uint32_t *s_total = s_next + 4u * digits, *s_here = s_total + digits;
+    for (uint32_t d = t; d < digits; d += kThreads) {
+        uint32_t total = 0u, here = 0u;
+        for (uint32_t tile = 0; tile < s.tiles; tile += 16u) {
+            uint32_t n[16];
+#pragma unroll
+            for (uint32_t q = 0; q < 16u; ++q) n[q] = tile + q < s.tiles ? s.counts[(uint64_t)(tile + q) * digits + d] : 0u;
+#pragma unroll
+            for (uint32_t q = 0; q < 16u; ++q) {
+                total += n[q];
+                here += tile + q < blockIdx.x ? n[q] : 0u;
+            }
         }
+        s_total[d] = total;
+        s_here[d] = here;
+    }
+    __syncthreads();
+    const uint32_t each = (digits + kThreads - 1u) / kThreads, d0 = t * each < digits ? t * each : digits, d1 = digits - d0 < each ? digits : d0 + each;
+    uint32_t total = 0u;
+    for (uint32_t d = d0; d < d1; ++d) total += s_total[d];
+    uint32_t at = sum_before(total, s_wave);
+    for (uint32_t d = d0; d < d1; ++d) {
+        uint32_t here = at + s_here[d];
+        at += s_total[d];
         for (uint32_t w = 0; w < 4u; ++w) {
             const uint32_t n = s_next[w * digits + d];
             s_next[w * digits + d] = here;
@@ -195,7 +232,8 @@ __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(EmbedArgs a, Sor
 
 // Up to kFew tokens: the whole sort in one workgroup, in LDS, 8 bits at a time.
 constexpr uint32_t kFew = 4096, kFewThreads = 1024;
-__global__ __launch_bounds__(kFewThreads) void sort_few_kernel(EmbedArgs a, uint32_t* keys_out, uint32_t* places_out, uint32_t key_bits) {
+__global__ __launch_bounds__(kFewThreads) void sort_few_kernel(EmbedArgs a, uint32_t* keys_out, uint32_t* places_out, uint32_t key_bits, ZeroShare z) {
+    if (zeroes(a, z, 1u)) return;
     constexpr uint32_t kWaves = kFewThreads / 64u;
     __shared__ uint32_t s_key[2][kFew], s_place[2][kFew], s_next[kWaves][256], s_wave[kWaves];
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6;
@@ -332,7 +370,7 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
     float sum[8] = {};
     float* part = s.parts + (uint64_t)p * s.pitch + d;
     auto keep = [&](float* to) { Row8<false>::store(to, sum); };
-    constexpr uint32_t kAhead = 4;
+    constexpr uint32_t kAhead = 8;
     for (uint32_t i = begin; i < end; i += kAhead) {
         uint32_t k[kAhead];
         float v[kAhead][8];
@@ -372,35 +410,39 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, SumAr
     const uint32_t d = (slice * s.lanes + threadIdx.x % s.lanes) * 8u;
     if (p + 1u >= s.pieces || d >= a.dim) return;
     const uint32_t begin = p * s.piece, end = begin + s.piece, key = s.keys[end - 1u];
-    if (key >= a.vocab || s.keys[end] != key) return;                                        // nothing goes on
-    if (s.keys[begin] == key && begin != 0u && s.keys[begin - 1u] == key) return;            // it has begun before
-    const uint32_t last = (lower_bound(s.keys, a.count, key + 1u) - 1u) / s.piece;
+    const uint32_t after = s.keys[end], first_key = s.keys[begin], before = s.keys[begin != 0u ? begin - 1u : 0u];
+    if (key >= a.vocab || after != key) return;                            // nothing goes on
+    if (first_key == key && begin != 0u && before == key) return;          // it has begun before
     float sum[8];
     load_row<false>(s.parts, ((uint64_t)s.pieces + p) * s.pitch + d, 8u, sum);
-    for (uint32_t q = p + 1u; q <= last; q += 8u) {
+    bool more = true;
+    for (uint32_t q = p + 1u; more && q < s.pieces; q += 8u) {   // pieces that begin with the run, 8 at a time
         float v[8][8];
+        uint32_t first[8];
 #pragma unroll
-        for (uint32_t r = 0; r < 8u; ++r)
-            load_row<false>(s.parts, (uint64_t)(q + r <= last ? q + r : last) * s.pitch + d, 8u, v[r]);
+        for (uint32_t r = 0; r < 8u; ++r) {
+            const uint32_t i = q + r < s.pieces ? q + r : s.pieces - 1u;
+            first[r] = s.keys[i * s.piece];
+            load_row<false>(s.parts, (uint64_t)i * s.pitch + d, 8u, v[r]);
+        }
 #pragma unroll
-        for (uint32_t r = 0; r < 8u; ++r)
-            if (q + r <= last)
+        for (uint32_t r = 0; r < 8u; ++r) {
+            more = more && q + r < s.pieces && first[r] == key;
+            if (more)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += v[r][e];
+        }
     }
     finish_row<OUT>(a, key, d, a.dim - d, sum);
 }
 
 // No tokens at all: zeros.
 template <bool OUT>
-__global__ __launch_bounds__(kThreads) void embed_zero_kernel(EmbedArgs a, uint32_t pieces) {
-    const uint64_t total = (uint64_t)a.vocab * pieces, step = (uint64_t)gridDim.x * kThreads;
-    const float zero[8] = {};
-    for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
-        const uint32_t d = (uint32_t)(i % pieces) * 8u;
-        store_row<OUT>(a.out, i / pieces * a.ld_out + d, a.dim - d, zero);
-    }
+__global__ __launch_bounds__(kThreads) void embed_zero_kernel(EmbedArgs a) {
+    zero_rows<OUT>(a, 0u, a.vocab, blockIdx.x, gridDim.x);
 }
+
+constexpr uint32_t kZeroGroups = 1024;   // workgroups that write zeros beside others
 
 uint32_t grid_for(uint64_t threads) {
     const uint64_t blocks = (threads + kThreads - 1u) / kThreads;
@@ -459,9 +501,8 @@ uint64_t embed_backward_workspace_bytes(uint64_t count, uint64_t vocab, uint64_t
 
 hipError_t launch_embed_backward(const EmbedArgs& a, hipStream_t stream) {
     if (a.count == 0u) {
-        const uint32_t pieces = (a.dim + 7u) / 8u, grid = grid_for((uint64_t)a.vocab * pieces);
-        if (a.out_bf16) embed_zero_kernel<true><<<grid, kThreads, 0, stream>>>(a, pieces);
-        else embed_zero_kernel<false><<<grid, kThreads, 0, stream>>>(a, pieces);
+        if (a.out_bf16) embed_zero_kernel<true><<<kZeroGroups, kThreads, 0, stream>>>(a);
+        else embed_zero_kernel<false><<<kZeroGroups, kThreads, 0, stream>>>(a);
         return hipGetLastError();
     }
     const EmbedPlan p = plan_for(a.count, a.vocab, a.dim);
@@ -475,8 +516,15 @@ hipError_t launch_embed_backward(const EmbedArgs& a, hipStream_t stream) {
     s.pieces = p.pieces;
     s.lanes = p.lanes;
     s.slices = p.slices;
+    // Far fewer tokens than rows: the sorting launches, which leave most of the device idle, zero the whole table beside it (rows that
+    // get a gradient are written twice).  Otherwise the summing launch zeroes the rows that get none.
+    const bool zero_first = !a.accumulate && a.count < a.vocab / 2u;
+    const uint32_t launches = a.count <= kFew ? 1u : 2u * p.passes, zeroers = zero_first ? kZeroGroups : 0u;
+    auto share = [&](uint32_t launch) {
+        return ZeroShare{(uint32_t)((uint64_t)a.vocab * launch / launches), (uint32_t)((uint64_t)a.vocab * (launch + 1u) / launches)};
+    };
     if (a.count <= kFew) {
-        sort_few_kernel<<<1, kFewThreads, 0, stream>>>(a, list[0], list[1], p.key_bits);
+        sort_few_kernel<<<1u + zeroers, kFewThreads, 0, stream>>>(a, list[0], list[1], p.key_bits, share(0));
         s.keys = list[0];
         s.places = list[1];
     } else {
@@ -490,15 +538,16 @@ hipError_t launch_embed_backward(const EmbedArgs& a, hipStream_t stream) {
             sort.tile = p.tile;
             sort.shift = pass * p.bits;
             sort.bits = p.bits;
-            sort_count_kernel<<<p.tiles, kThreads, 4u << p.bits, stream>>>(a, sort);
-            sort_scatter_kernel<<<p.tiles, kThreads, 16u << p.bits, stream>>>(a, sort);
+            sort.tiles = p.tiles;
+            sort_count_kernel<<<p.tiles + zeroers, kThreads, 4u << p.bits, stream>>>(a, sort, share(2u * pass));
+            sort_scatter_kernel<<<p.tiles + zeroers, kThreads, 24u << p.bits, stream>>>(a, sort, share(2u * pass + 1u));
             s.keys = sort.keys_out;
             s.places = sort.places_out;
         }
     }
     const uint64_t groups = (uint64_t)p.pieces * p.slices * p.lanes;
     s.sum_groups = (uint32_t)((groups + kThreads - 1u) / kThreads);
-    const uint32_t zero_rows = (a.vocab + kZeroRows - 1u) / kZeroRows, zero_groups = a.accumulate ? 0u : zero_rows < (1u << 20) ? zero_rows : 1u << 20;
+    const uint32_t zero_rows = (a.vocab + kZeroRows - 1u) / kZeroRows, zero_groups = a.accumulate || zero_first ? 0u : zero_rows < (1u << 20) ? zero_rows : 1u << 20;
     auto out = [&](auto O) {
         constexpr bool OUT = decltype(O)::value;
         if (a.in_bf16) embed_sum_kernel<true, OUT><<<s.sum_groups + zero_groups, kThreads, 0, stream>>>(a, s);
