@@ -100,7 +100,7 @@ template <int FA, int FB, bool EXACT, int SOURCE, int MF, int NF, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void fp8_direct_kernel(Fp8DirectArgs a, uint32_t tiles_m, uint32_t tiles_n) {
     constexpr uint32_t kCols = 16u * NF, kPitch = kCols + 4u;
     constexpr uint32_t kAhead = NF > 1 ? 2u : 4u;          // blocks of a wave in flight
-    constexpr uint32_t kAheadX = SOURCE == 1 ? 2u : 1u;    // blocks of x held unquantized (its rows come from the cache)
+    constexpr uint32_t kAheadX = SOURCE == 1 ? 2u : 1u;    // blocks of x held unquantized (128 registers: two workgroups to a compute unit)
     __shared__ __attribute__((aligned(16))) float s_sum[WAVES][16][kPitch];
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6, r = lane & 15u, g = lane >> 4;
     uint32_t tm, tn;
@@ -122,9 +122,20 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_direct_kernel(Fp8DirectArgs a,
         i32x8 vb[NF][kAhead], va[SOURCE ? 1 : MF][kAhead];
         uint32_t eb[NF][kAhead], ea[SOURCE ? 1 : MF][kAhead];
         Raw<SOURCE == 1, FA == 1> raw[SOURCE ? MF : 1][kAheadX];
+        auto load_x = [&](uint32_t first) {
+#pragma unroll
+            for (uint32_t p = 0; p < kAheadX; ++p)
+#pragma unroll
+                for (int f = 0; f < MF; ++f) {
+                    const uint32_t j = j0 + (first + p) * WAVES, k = j * 128u + 16u * g;
+                    if (j < end) raw[f][p].load(a.x, (uint64_t)m[f] * a.ldx + k, (int32_t)a.K - (int32_t)k);
+                }
+        };
+        if constexpr (SOURCE != 0) load_x(0);   // (before B: what is loaded first arrives first, and there is work to do on it)
 #pragma unroll
         for (uint32_t q = 0; q < kAhead; ++q) {
-            const uint32_t j = j0 + q * WAVES < end ? j0 + q * WAVES : j0;   // (behind the last block: loaded, not used)
+            const uint32_t ahead = j0 + q * WAVES, j = ahead < end ? ahead : j0;
+            if (NF == 1 && ahead >= end) continue;   // (tiles: loaded, not used, which keeps the loads in one run)
 #pragma unroll
             for (int i = 0; i < NF; ++i) {
                 vb[i][q] = load32(a.b + n[i] * ld + j * 128u + 16u * g);
@@ -141,15 +152,7 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_direct_kernel(Fp8DirectArgs a,
 #pragma unroll
         for (uint32_t q = 0; q < kAhead; ++q) {
             if constexpr (SOURCE != 0) {
-                if (q % kAheadX == 0u) {
-#pragma unroll
-                    for (uint32_t p = 0; p < kAheadX; ++p)
-#pragma unroll
-                        for (int f = 0; f < MF; ++f) {
-                            const uint32_t j = j0 + (q + p) * WAVES, k = j * 128u + 16u * g;
-                            if (j < end) raw[f][p].load(a.x, (uint64_t)m[f] * a.ldx + k, (int32_t)a.K - (int32_t)k);
-                        }
-                }
+                if (q != 0u && q % kAheadX == 0u) load_x(q);
             }
             if (j0 + q * WAVES >= end) continue;
 #pragma unroll
@@ -197,6 +200,8 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_direct_kernel(Fp8DirectArgs a,
     }
 }
 
+constexpr int kFewWaves = 8;
+
 using I0 = std::integral_constant<int, 0>;
 using I1 = std::integral_constant<int, 1>;
 using I2 = std::integral_constant<int, 2>;
@@ -224,7 +229,7 @@ hipError_t launch_fp8_direct(const Fp8DirectArgs& args, hipStream_t stream) {
         constexpr int A = decltype(FA)::value, B = decltype(FB)::value;
         constexpr bool E = decltype(EXACT)::value;
         auto go = [&](auto S) {
-            fp8_direct_kernel<A, B, E, decltype(S)::value, 1, 1, 8><<<grid, 512, 0, stream>>>(a, tiles_m, tiles_n);
+            fp8_direct_kernel<A, B, E, decltype(S)::value, 1, 1, kFewWaves><<<grid, 64 * kFewWaves, 0, stream>>>(a, tiles_m, tiles_n);
         };
         if (!few) fp8_direct_kernel<A, B, E, 0, 4, 4, 4><<<grid, 256, 0, stream>>>(a, tiles_m, tiles_n);
         else if (a.source == 0u) go(I0{});

@@ -311,7 +311,7 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8MatmulArgs a, uint32_t
         const uint32_t m = (uint32_t)(i / pieces), n = (uint32_t)(i % pieces) * 4u;
         const float* at = a.workspace + m * pitch + n;
         float4 v = *reinterpret_cast<const float4*>(at);
-#pragma unroll 4
+#pragma unroll 8
         for (uint32_t p = 1; p < parts; ++p) {
             const float4 w = *reinterpret_cast<const float4*>(at + p * a.M * pitch);
             v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
