@@ -57,13 +57,14 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         }
     }
     uint32_t base = wave * 1024u;
-    auto fetch = [&](uint8_t* s, auto unit, uint32_t step) {
-        constexpr uint32_t u = decltype(unit)::value;
-        asm volatile("" : "+s"(base));   // (all places in LDS, kept across the loop, would not fit the scalar registers)
+    auto fetch_one = [&](uint8_t* s, uint32_t unit, uint32_t i, uint32_t step) __attribute__((always_inline)) {
         const int k = (int)((first + (step < steps ? step : 0u)) * kStep);   // (behind the last step: not used)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(unit < 2u ? src_a : src_b, (lds_void*)(s + base + i * 4096u), 16, (int)off[unit][i], k, 0, 0);
+    };
+    auto fetch = [&](uint8_t* s, uint32_t unit, uint32_t step) __attribute__((always_inline)) {
+        asm volatile("" : "+s"(base));   // (all places in LDS, kept across the loop, would not fit the scalar registers)
 #pragma unroll
-        for (uint32_t i = 0; i < MF; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(u < 2u ? src_a : src_b, (lds_void*)(s + base + i * 4096u), 16, (int)off[u][i], k, 0, 0);
+        for (uint32_t i = 0; i < MF; ++i) fetch_one(s, unit, i, step);
     };
 
     // LDS -> registers.  Rows of B are taken in the order with bits 2 and 3 exchanged, which gives a lane 8
@@ -71,18 +72,17 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     const uint32_t xb = (x & 0x13u) | (x & 4u) << 1 | (x & 8u) >> 1;
     const uint32_t at_a = (wm * 16u * MF + x) * kStep + (((2u * h) ^ ((x >> 1) & 7u)) << 4);
     const uint32_t at_b = (wn * 16u * MF + xb) * kStep + (((2u * h) ^ ((x >> 1) & 7u)) << 4);
-    auto read = [&](auto first, uint32_t half, i32x8 (&fa)[MF], i32x8 (&fb)[NF]) {   // first: the step's first unit
-        constexpr uint32_t u = decltype(first)::value;
+    auto read_one = [&](uint32_t u, uint32_t half, uint32_t f, i32x8 (&fa)[MF], i32x8 (&fb)[NF]) __attribute__((always_inline)) {   // u: the step's first unit
         auto piece = [&](const uint8_t* s, uint32_t at) {
             const uint4 lo = *reinterpret_cast<const uint4*>(s + at), hi = *reinterpret_cast<const uint4*>(s + (at ^ 16u));
             return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         };
+        if (f < MF) fa[f] = piece(slots[(u + f / (MF / 2u)) % kSlots], (at_a ^ (half << 6)) + f % (MF / 2u) * 32u * kStep);
+        else fb[f - MF] = piece(slots[(u + 2u + (f - MF) / (NF / 2u)) % kSlots], (at_b ^ (half << 6)) + (f - MF) % (NF / 2u) * 32u * kStep);
+    };
+    auto read = [&](uint32_t u, uint32_t half, i32x8 (&fa)[MF], i32x8 (&fb)[NF]) __attribute__((always_inline)) {
 #pragma unroll
-        for (uint32_t f = 0; f < MF; ++f)
-            fa[f] = piece(slots[(u + f / (MF / 2u)) % kSlots], (at_a ^ (half << 6)) + f % (MF / 2u) * 32u * kStep);
-#pragma unroll
-        for (uint32_t f = 0; f < NF; ++f)
-            fb[f] = piece(slots[(u + 2u + f / (NF / 2u)) % kSlots], (at_b ^ (half << 6)) + f % (NF / 2u) * 32u * kStep);
+        for (uint32_t f = 0; f < MF + NF; ++f) read_one(u, half, f, fa, fb);
     };
 
     // scale words: four blocks each
@@ -115,28 +115,6 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         for (int j = 0; j < NF; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    auto multiply = [&](const i32x8 (&fa)[MF], const i32x8 (&fb)[NF]) {
-        if constexpr (EXACT) {
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                bf16x8 wa[MF], wb[NF];
-#pragma unroll
-                for (int i = 0; i < MF; ++i) wa[i] = fp8_widen<FA>(fa[i][2 * p], fa[i][2 * p + 1], fp8_scale(sa[i]));
-#pragma unroll
-                for (int j = 0; j < NF; ++j) wb[j] = fp8_widen<FB>(fb[j][2 * p], fb[j][2 * p + 1], fp8_scale(sb[j]));
-#pragma unroll
-                for (int i = 0; i < MF; ++i)
-#pragma unroll
-                    for (int j = 0; j < NF; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j], wa[i], acc[i][j], 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < MF; ++i)
-#pragma unroll
-                for (int j = 0; j < NF; ++j) acc[i][j] = fp8_mfma32<FB, FA>(fb[j], fa[i], acc[i][j], sb[j], sa[i]);
-        }
-    };
     // Keeps the products of a half between two points of the program: its codes are taken from here on, its sums are
     // formed here (a product is free to move across a barrier otherwise, and three halves of codes would be held).
     auto from_here = [&](i32x8 (&fa)[MF], i32x8 (&fb)[NF]) {
@@ -158,50 +136,84 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     // it fetched of the next step, with the 2 units fetched last still on their way: from there on two units of the step
     // after the next one, and in the next first half two of the one behind it, go where the step's were.
     i32x8 fa0[MF], fb0[NF], fa1[MF], fb1[NF];
-    auto order = [&]() {   // reads from LDS among the first products, then fetches
+    // What is multiplied and what is widened to bfloat16 for the next 16 k meanwhile.
+    bf16x8 wide[2][EXACT ? MF + NF : 1];
+    auto widen = [&](uint32_t to, uint32_t f, uint32_t p, const i32x8 (&fa)[MF], const i32x8 (&fb)[NF], const uint32_t (&ea)[MF],
+                     const uint32_t (&eb)[NF]) __attribute__((always_inline)) {
+        if (f < MF) wide[to][f] = fp8_widen<FA>(fa[f][2 * p], fa[f][2 * p + 1], fp8_scale(ea[f]));
+        else wide[to][f] = fp8_widen<FB>(fb[f - MF][2 * p], fb[f - MF][2 * p + 1], fp8_scale(eb[f - MF]));
+    };
+    // A half: the products of (fa, fb) with the scales sa, sb, while (ga, gb), the next half with the scales ea, eb, is read
+    // from the step whose first unit is u, and two units from `unit` on, of two steps ahead, are fetched into the slots from `to` on.
+    auto half_step = [&](i32x8 (&fa)[MF], i32x8 (&fb)[NF], uint32_t u, uint32_t half, i32x8 (&ga)[MF], i32x8 (&gb)[NF],
+                         const uint32_t (&ea)[MF], const uint32_t (&eb)[NF], uint32_t to, uint32_t unit, uint32_t step) __attribute__((always_inline)) {
+        from_here(fa, fb);
+        if constexpr (EXACT) {
+            constexpr uint32_t kOperands = MF + NF, kProducts = MF * NF / kOperands;   // products of 16 k beside each widened operand
+            asm volatile("" : "+s"(base));
 #pragma unroll
-        for (int i = 0; i < (MF + NF) / 2; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, EXACT ? MF : 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-        }
+            for (uint32_t p = 0; p < 4; ++p)
 #pragma unroll
-        for (int i = 0; i < 2 * MF; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, EXACT ? MF : 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+                for (uint32_t f = 0; f < kOperands; ++f) {
+                    if (p < 3) widen((p + 1u) & 1u, f, p + 1u, fa, fb, sa, sb);
+                    else widen(0, f, 0, ga, gb, ea, eb);
+#pragma unroll
+                    for (uint32_t q = f * kProducts; q < (f + 1u) * kProducts; ++q)
+                        acc[q / NF][q % NF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[p & 1u][MF + q % NF], wide[p & 1u][q / NF], acc[q / NF][q % NF], 0, 0, 0);
+                    if (p == 0) read_one(u, half, f, ga, gb);
+                    if (p == 3) asm volatile("" : "+v"(wide[0][f]));   // (here, not in the next half)
+                    if (p == 1) fetch_one(slots[(to + f / MF) % kSlots], unit + f / MF, f % MF, step);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        } else {
+            read(u, half, ga, gb);
+            fetch(slots[to % kSlots], unit, step);
+            fetch(slots[(to + 1u) % kSlots], unit + 1u, step);
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int j = 0; j < NF; ++j) acc[i][j] = fp8_mfma32<FB, FA>(fb[j], fa[i], acc[i][j], sb[j], sa[i]);
+            // four reads behind each of the first products, then fetches
+#pragma unroll
+            for (int i = 0; i < (MF + NF) / 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * MF; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+            }
         }
         up_to_here();
     };
-    auto step = [&](auto phase, uint32_t k) {   // phase: k mod 5
+    auto step = [&](auto phase, uint32_t k) __attribute__((always_inline)) {   // phase: k mod 5
         constexpr uint32_t u = 4u * decltype(phase)::value;
-        from_here(fa0, fb0);
-        read(std::integral_constant<uint32_t, u>{}, 1, fa1, fb1);
-        fetch(slots[(u + 8u) % kSlots], std::integral_constant<uint32_t, 0>{}, k + 2u);
-        fetch(slots[(u + 9u) % kSlots], std::integral_constant<uint32_t, 1>{}, k + 2u);
-        multiply(fa0, fb0);
-        order();
+        half_step(fa0, fb0, u, 1, fa1, fb1, sa, sb, u + 8u, 0, k + 2u);
         constexpr uint32_t kLeft = 2u * MF;
         __builtin_amdgcn_s_waitcnt((kLeft & 15u) | (kLeft >> 4) << 14 | 7u << 4);   // vmcnt(kLeft) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        from_here(fa1, fb1);
-        read(std::integral_constant<uint32_t, u + 4u>{}, 0, fa0, fb0);
-        fetch(slots[(u + 10u) % kSlots], std::integral_constant<uint32_t, 2>{}, k + 2u);
-        fetch(slots[(u + 11u) % kSlots], std::integral_constant<uint32_t, 3>{}, k + 2u);
-        multiply(fa1, fb1);
-        order();
+        uint32_t ta[MF], tb[NF];   // the next step's scales
         if (((first + k) & 3u) == 3u) {   // (moved, not renamed: a load that may be on its way would be waited for in every step)
 #pragma unroll
-            for (int i = 0; i < MF; ++i) asm volatile("v_mov_b32 %0, %1" : "=v"(sa[i]) : "v"(next_a[i]));
+            for (int i = 0; i < MF; ++i) asm volatile("v_mov_b32 %0, %1" : "=v"(ta[i]) : "v"(next_a[i]));
 #pragma unroll
-            for (int j = 0; j < NF; ++j) asm volatile("v_mov_b32 %0, %1" : "=v"(sb[j]) : "v"(next_b[j]));
+            for (int j = 0; j < NF; ++j) asm volatile("v_mov_b32 %0, %1" : "=v"(tb[j]) : "v"(next_b[j]));
             const uint32_t w = ((first + k) >> 2) + 2u;
             scales(w < words ? w : 0u, next_a, next_b);
         } else {
 #pragma unroll
-            for (int i = 0; i < MF; ++i) sa[i] >>= 8;
+            for (int i = 0; i < MF; ++i) ta[i] = sa[i] >> 8;
 #pragma unroll
-            for (int j = 0; j < NF; ++j) sb[j] >>= 8;
+            for (int j = 0; j < NF; ++j) tb[j] = sb[j] >> 8;
         }
+        __builtin_amdgcn_sched_barrier(0);
+        half_step(fa1, fb1, u + 4u, 0, fa0, fb0, ta, tb, u + 10u, 2, k + 2u);
+#pragma unroll
+        for (int i = 0; i < MF; ++i) sa[i] = ta[i];
+#pragma unroll
+        for (int j = 0; j < NF; ++j) sb[j] = tb[j];
     };
     scales(word0, sa, sb);
     scales(word0 + 1u < words ? word0 + 1u : 0u, next_a, next_b);
@@ -209,19 +221,22 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     for (int i = 0; i < MF; ++i) sa[i] >>= 8u * (first & 3u);
 #pragma unroll
     for (int j = 0; j < NF; ++j) sb[j] >>= 8u * (first & 3u);
-    fetch(s0, std::integral_constant<uint32_t, 0>{}, 0);
-    fetch(s1, std::integral_constant<uint32_t, 1>{}, 0);
-    fetch(s2, std::integral_constant<uint32_t, 2>{}, 0);
-    fetch(s3, std::integral_constant<uint32_t, 3>{}, 0);
-    fetch(s4, std::integral_constant<uint32_t, 0>{}, 1);
-    fetch(s5, std::integral_constant<uint32_t, 1>{}, 1);
-    fetch(s6, std::integral_constant<uint32_t, 2>{}, 1);
-    fetch(s7, std::integral_constant<uint32_t, 3>{}, 1);
+    fetch(s0, 0, 0);
+    fetch(s1, 1, 0);
+    fetch(s2, 2, 0);
+    fetch(s3, 3, 0);
+    fetch(s4, 0, 1);
+    fetch(s5, 1, 1);
+    fetch(s6, 2, 1);
+    fetch(s7, 3, 1);
     constexpr uint32_t kNext = 4u * MF;
     __builtin_amdgcn_s_waitcnt((kNext & 15u) | (kNext >> 4) << 14 | 0xF70u);   // vmcnt(kNext): step 0
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    read(std::integral_constant<uint32_t, 0>{}, 0, fa0, fb0);
+    read(0, 0, fa0, fb0);
+    if constexpr (EXACT)
+#pragma unroll
+        for (uint32_t f = 0; f < MF + NF; ++f) widen(0, f, 0, fa0, fb0, sa, sb);
     __builtin_amdgcn_sched_barrier(0);
     uint32_t k = 0;
     for (; k + 4u < steps; k += 5u) {
