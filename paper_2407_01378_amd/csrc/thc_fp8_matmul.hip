@@ -11,7 +11,8 @@
 namespace thc {
 namespace {
 
-constexpr uint32_t kStep = 128, kHalf = 64;
+constexpr uint32_t kStep = 128;
+constexpr uint32_t kUnits = 256;   // compute units (a multiple of the dies, so that a workgroup's tiles are its die's)
 constexpr uint64_t kMaxGrid = 1ull << 23;   // workgroups of 256 threads: 2^31 threads
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -20,6 +21,7 @@ template <int FA, int FB, bool EXACT, int MF, int NF>
 __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs a, uint32_t tiles_m, uint32_t tiles_n) {
     constexpr uint32_t BM = 64u * MF, BN = 64u * NF;
     static_assert(MF == NF, "the four units of a step have one size");
+    constexpr bool kWalks = MF == 4;   // one workgroup on a compute unit, which goes from tile to tile (two, a tile each, otherwise)
     // A step's codes are four units, the even and the odd halves of the waves' rows of A and of B; ten units fit LDS.  (Arrays of
     // their own: that a fetch to one does not touch what is read from another has to be seen.)
     constexpr uint32_t kUnitRows = 32u * MF, kUnit = kUnitRows * kStep, kSlots = 10;
@@ -28,38 +30,52 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     uint8_t* const slots[kSlots] = {s0, s1, s2, s3, s4, s5, s6, s7, s8, s9};
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const uint32_t x = lane & 31u, h = lane >> 5, wm = wave & 1u, wn = wave >> 1;
-    uint32_t tm, tn;
-    place_tile(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
     // this workgroup's part of the blocks along k
     const uint32_t blocks = (a.K + kStep - 1u) / kStep, ld = blocks * kStep, first = blockIdx.y * a.share;
     const uint32_t steps = blocks - first < a.share ? blocks - first : a.share;
-    const uint32_t m0 = tm * BM, n0 = tn * BN;
 
     // memory -> LDS: a wave moves 8 rows (whole lines of memory) at a time, lane l the piece of 16 codes that belongs at place
     // l % 8 of row l / 8.  Piece c of a row lies at place c ^ key: two rows fill all banks, and of 16 lanes that read
     // one piece of their rows at a time no two may share a place in rows of the same parity.  key = bits 1, 2, 3 of the
     // row, in the order in which lanes take the rows.
-    const uint32_t left_m = a.M - m0, left_n = a.N - n0;
-    const uint32_t rows_m = left_m < BM ? left_m : BM, rows_n = left_n < BN ? left_n : BN;
-    const auto src_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.a + (uint64_t)m0 * ld), 0, rows_m * ld, 0x00020000);
-    const auto src_b = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.b + (uint64_t)n0 * ld), 0, rows_n * ld, 0x00020000);
-    uint32_t off[4][MF];
-    const uint32_t key_a = lane >> 4 | (wave & 1u) << 2, key_b = ((lane >> 4) & 1u) | (wave & 1u) << 1 | (lane >> 5) << 2;
+    uint32_t m0, n0, rows_m, rows_n, off[4][MF];
+    uint32_t row_a[MF], row_b[NF];   // of the scales, in bytes from the tile's first row
+    auto go_to = [&](uint32_t tile) __attribute__((always_inline)) {
+        uint32_t tm, tn, l = lane;
+        asm volatile("" : "+v"(l));   // (worked out for each tile, not kept)
+        const uint32_t x = l & 31u, xb = (x & 0x13u) | (x & 4u) << 1 | (x & 8u) >> 1;   // (rows of B: bits 2 and 3 exchanged)
+        const uint32_t key_a = l >> 4 | (wave & 1u) << 2, key_b = ((l >> 4) & 1u) | (wave & 1u) << 1 | (l >> 5) << 2;
+        place_tile(tile, tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
+        m0 = tm * BM, n0 = tn * BN;
+        rows_m = a.M - m0 < BM ? a.M - m0 : BM, rows_n = a.N - n0 < BN ? a.N - n0 : BN;
 #pragma unroll
-    for (uint32_t i = 0; i < MF; ++i) {
-        const uint32_t q = 8u * (wave + 4u * i) + (lane >> 3);   // row of the unit
-        const uint32_t r = q / (16u * MF) * (32u * MF) + q % (16u * MF);
+        for (uint32_t i = 0; i < MF; ++i) {
+            const uint32_t q = 8u * (wave + 4u * i) + (l >> 3);   // row of the unit
+            const uint32_t r = q / (16u * MF) * (32u * MF) + q % (16u * MF);
 #pragma unroll
-        for (uint32_t u = 0; u < 2u; ++u) {
-            const uint32_t ru = r + u * 16u * MF;
-            off[u][i] = (ru < rows_m ? ru : rows_m - 1u) * ld + (((lane & 7u) ^ key_a) << 4);
-            off[2u + u][i] = (ru < rows_n ? ru : rows_n - 1u) * ld + (((lane & 7u) ^ key_b) << 4);
+            for (uint32_t u = 0; u < 2u; ++u) {
+                const uint32_t ru = r + u * 16u * MF;
+                off[u][i] = (ru < rows_m ? ru : rows_m - 1u) * ld + (((l & 7u) ^ key_a) << 4);
+                off[2u + u][i] = (ru < rows_n ? ru : rows_n - 1u) * ld + (((l & 7u) ^ key_b) << 4);
+            }
         }
-    }
+#pragma unroll
+        for (uint32_t f = 0; f < MF; ++f) {
+            const uint32_t r = wm * 32u * MF + f * 32u + x;
+            row_a[f] = 4u * (r < rows_m ? r : rows_m - 1u);
+        }
+#pragma unroll
+        for (uint32_t f = 0; f < NF; ++f) {
+            const uint32_t r = wn * 32u * NF + f * 32u + xb;
+            row_b[f] = 4u * (r < rows_n ? r : rows_n - 1u);
+        }
+    };
     uint32_t base = wave * 1024u;
     auto fetch_one = [&](uint8_t* s, uint32_t unit, uint32_t i, uint32_t step) __attribute__((always_inline)) {
         const int k = (int)((first + (step < steps ? step : 0u)) * kStep);   // (behind the last step: not used)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(unit < 2u ? src_a : src_b, (lds_void*)(s + base + i * 4096u), 16, (int)off[unit][i], k, 0, 0);
+        const auto src = unit < 2u ? __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.a + (uint64_t)m0 * ld), 0, rows_m * ld, 0x00020000)
+                                   : __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.b + (uint64_t)n0 * ld), 0, rows_n * ld, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(s + base + i * 4096u), 16, (int)off[unit][i], k, 0, 0);
     };
     auto fetch = [&](uint8_t* s, uint32_t unit, uint32_t step) __attribute__((always_inline)) {
         asm volatile("" : "+s"(base));   // (all places in LDS, kept across the loop, would not fit the scalar registers)
@@ -86,17 +102,6 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     };
 
     // scale words: four blocks each
-    uint32_t row_a[MF], row_b[NF];   // in bytes from the tile's first row
-#pragma unroll
-    for (uint32_t f = 0; f < MF; ++f) {
-        const uint32_t r = wm * 32u * MF + f * 32u + x;
-        row_a[f] = 4u * (r < rows_m ? r : rows_m - 1u);
-    }
-#pragma unroll
-    for (uint32_t f = 0; f < NF; ++f) {
-        const uint32_t r = wn * 32u * NF + f * 32u + xb;
-        row_b[f] = 4u * (r < rows_n ? r : rows_n - 1u);
-    }
     auto scales = [&](uint32_t word, uint32_t (&wa)[MF], uint32_t (&wb)[NF]) {
         const uint8_t* pa = reinterpret_cast<const uint8_t*>(a.a_scales + (uint64_t)word * a.M + m0);
         const uint8_t* pb = reinterpret_cast<const uint8_t*>(a.b_scales + (uint64_t)word * a.N + n0);
@@ -109,12 +114,6 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
     const uint32_t word0 = first >> 2, words = (blocks + 3u) / 4u;
     uint32_t sa[MF], sb[NF], next_a[MF], next_b[NF];
     f32x16 acc[MF][NF];
-#pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     // Keeps the products of a half between two points of the program: its codes are taken from here on, its sums are
     // formed here (a product is free to move across a barrier otherwise, and three halves of codes would be held).
     auto from_here = [&](i32x8 (&fa)[MF], i32x8 (&fb)[NF]) {
@@ -187,11 +186,16 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         }
         up_to_here();
     };
+    // For s_waitcnt: all but the youngest operations on memory (63 at most are counted).
+    auto all_but = [](uint32_t left) {
+        const uint32_t n = left < 63u ? left : 63u;
+        return (n & 15u) | n >> 4 << 14;
+    };
     auto step = [&](auto phase, uint32_t k) __attribute__((always_inline)) {   // phase: k mod 5
         constexpr uint32_t u = 4u * decltype(phase)::value;
         half_step(fa0, fb0, u, 1, fa1, fb1, sa, sb, u + 8u, 0, k + 2u);
-        constexpr uint32_t kLeft = 2u * MF;
-        __builtin_amdgcn_s_waitcnt((kLeft & 15u) | (kLeft >> 4) << 14 | 7u << 4);   // vmcnt(kLeft) lgkmcnt(0)
+        if (!kWalks || u != 0u || k != 0u) __builtin_amdgcn_s_waitcnt(all_but(2u * MF) | 0xF70u);
+        __builtin_amdgcn_s_waitcnt(all_but(63u) | 0x070u);   // what was read
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         uint32_t ta[MF], tb[NF];   // the next step's scales
@@ -215,64 +219,46 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
 #pragma unroll
         for (int j = 0; j < NF; ++j) sb[j] = tb[j];
     };
-    scales(word0, sa, sb);
-    scales(word0 + 1u < words ? word0 + 1u : 0u, next_a, next_b);
-#pragma unroll
-    for (int i = 0; i < MF; ++i) sa[i] >>= 8u * (first & 3u);
-#pragma unroll
-    for (int j = 0; j < NF; ++j) sb[j] >>= 8u * (first & 3u);
-    fetch(s0, 0, 0);
-    fetch(s1, 1, 0);
-    fetch(s2, 2, 0);
-    fetch(s3, 3, 0);
-    fetch(s4, 0, 1);
-    fetch(s5, 1, 1);
-    fetch(s6, 2, 1);
-    fetch(s7, 3, 1);
-    constexpr uint32_t kNext = 4u * MF;
-    __builtin_amdgcn_s_waitcnt((kNext & 15u) | (kNext >> 4) << 14 | 0xF70u);   // vmcnt(kNext): step 0
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    read(0, 0, fa0, fb0);
-    if constexpr (EXACT)
-#pragma unroll
-        for (uint32_t f = 0; f < MF + NF; ++f) widen(0, f, 0, fa0, fb0, sa, sb);
-    __builtin_amdgcn_sched_barrier(0);
-    uint32_t k = 0;
-    for (; k + 4u < steps; k += 5u) {
-        step(std::integral_constant<uint32_t, 0>{}, k);
-        step(std::integral_constant<uint32_t, 1>{}, k + 1u);
-        step(std::integral_constant<uint32_t, 2>{}, k + 2u);
-        step(std::integral_constant<uint32_t, 3>{}, k + 3u);
-        step(std::integral_constant<uint32_t, 4>{}, k + 4u);
-    }
-    if (k < steps) step(std::integral_constant<uint32_t, 0>{}, k);
-    if (k + 1u < steps) step(std::integral_constant<uint32_t, 1>{}, k + 1u);
-    if (k + 2u < steps) step(std::integral_constant<uint32_t, 2>{}, k + 2u);
-    if (k + 3u < steps) step(std::integral_constant<uint32_t, 3>{}, k + 3u);
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // (what was fetched behind the last step)
-
-    // 32 rows of a wave at a time by way of LDS, so that a row leaves in whole lines: stored as the matrix unit holds them, two
-    // lanes to a row, the writes of all workgroups took the caches ten times as long.  Pieces of 16 bytes are kept at places
-    // exchanged by row, as above.  One of several parts keeps its sums in fp32, in rows with room up to a multiple of 8.
-    __builtin_amdgcn_s_barrier();   // (nothing is on its way to LDS any more)
-    auto emit = [&](auto wide, auto half, void* out, uint64_t pitch, uint32_t columns, bool add) {   // sums kept in fp32; bf16 results
-        constexpr bool kWide = decltype(wide)::value, kHalf16 = decltype(half)::value;
-        constexpr uint32_t kPieces = (kWide ? 8u : 4u) * NF, kEach = kWide ? 4u : 8u;   // of a row, and values of one
-        static_assert(32u * kPieces * 16u <= kUnit, "a strip fits a unit");
-        uint8_t* strip = wave == 0u ? s0 : wave == 1u ? s1 : wave == 2u ? s2 : s3;
-        auto place = [&](uint32_t r, uint32_t piece) {
+    auto begin = [&]() __attribute__((always_inline)) {   // a tile's first scales and two steps
+        scales(word0, sa, sb);
+        scales(word0 + 1u < words ? word0 + 1u : 0u, next_a, next_b);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(s0, 0, 0);
+        fetch(s1, 1, 0);
+        fetch(s2, 2, 0);
+        fetch(s3, 3, 0);
+        fetch(s4, 0, 1);
+        fetch(s5, 1, 1);
+        fetch(s6, 2, 1);
+        fetch(s7, 3, 1);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // 32 rows of a wave at a time by way of LDS, in the two units that the next tile's first steps leave free, so that a row leaves in
+    // whole lines: stored as the matrix unit holds them, two lanes to a row, the writes of all workgroups took the caches ten times
+    // as long.  Pieces of 16 bytes are kept at places exchanged by row, as above; fp32 sums leave in two halves of the columns.  One of
+    // several parts keeps its sums in fp32, in rows with room up to a multiple of 8.
+    auto emit = [&](auto wide, auto half, bool whole, uint32_t m1, uint32_t n1, void* out, uint64_t pitch, uint32_t columns, bool add) __attribute__((always_inline)) {
+        constexpr bool kWide = decltype(wide)::value, kHalf16 = decltype(half)::value;   // sums kept in fp32; bf16 results
+        constexpr uint32_t kPieces = 4u * NF, kEach = kWide ? 4u : 8u, kTurns = kWide ? 2u : 1u;   // of a strip's row, values of a piece
+        static_assert(32u * kPieces * 16u <= kUnit / 2u, "a strip fits half a unit");
+        uint8_t* strip = (wave < 2u ? s8 : s9) + (wave & 1u) * (kUnit / 2u);
+        auto place = [&](uint32_t r, uint32_t piece) __attribute__((always_inline)) {
             return reinterpret_cast<uint4*>(strip + (r * kPieces + (piece ^ (kPieces >= 16u ? r & 15u : (r >> 1) & 7u))) * 16u);
         };
-        const uint32_t nw = n0 + wn * 32u * NF;
+        uint32_t l = lane;   // (places are worked out here, in each variant by itself, not kept while products are formed)
+        asm volatile("; %1" : "+v"(l) : "n"(kWide + 2 * kHalf16));
+        asm volatile("s_nop 15\n s_nop 15");   // (the last products' results; the reads below are written out, else whole sums are copied and spilled)
+        const uint32_t x = l & 31u, h = l >> 5;
 #pragma unroll
-        for (uint32_t i = 0; i < MF; ++i) {
+        for (uint32_t turn = 0; turn < MF * kTurns; ++turn) {
+            const uint32_t i = turn / kTurns, j0 = turn % kTurns * NF, nw = n1 + wn * 32u * NF + j0 * 16u;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (uint32_t j = 0; j < 2u * NF; ++j) {
+            for (uint32_t j = 0; j < 2u * NF / kTurns; ++j) {
                 float v[8];
 #pragma unroll
-                for (uint32_t e = 0; e < 8u; ++e) v[e] = acc[i][j >> 1][8u * (j & 1u) + e];
+                for (uint32_t e = 0; e < 8u; ++e)
+                    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][(j0 + j) >> 1][8u * ((j0 + j) & 1u) + e]));
                 const uint32_t g = 2u * j + h;   // 8 columns
                 if (kWide) {
                     *place(x, 2u * g) = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
@@ -283,37 +269,106 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
+            const uint32_t r0 = l / kPieces, piece = l % kPieces, n = nw + piece * kEach, row = m1 + wm * 32u * MF + i * 32u + r0;
+            if (whole) {
+                uint8_t* at = static_cast<uint8_t*>(out) + (row * pitch + n) * (kHalf16 ? 2u : 4u);
+                const uint64_t step = 64u / kPieces * pitch * (kHalf16 ? 2u : 4u);
+                uint4 w[kPieces / 2u];
 #pragma unroll
-            for (uint32_t it = 0; it < kPieces / 2u; ++it) {
-                const uint32_t r = it * (64u / kPieces) + lane / kPieces, piece = lane % kPieces;
-                const uint32_t m = m0 + wm * 32u * MF + i * 32u + r, n = nw + piece * kEach;
-                const uint4 w = *place(r, piece);
-                if (m >= a.M || n >= columns) continue;
-                uint8_t* at = static_cast<uint8_t*>(out) + (m * pitch + n) * (kHalf16 ? 2u : 4u);
-                if (kWide) {
-                    store4<kHalf16>(at, f32x4{__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)}, columns - n, add);
-                } else if (n + 8u <= columns) {
-                    store16(at, w);
-                } else {
-                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+                for (uint32_t it = 0; it < kPieces / 2u; ++it) w[it] = *place(r0 + it * (64u / kPieces), piece);
 #pragma unroll
-                    for (uint32_t e = 0; e < 7u; ++e)
-                        if (n + e < columns) reinterpret_cast<uint16_t*>(at)[e] = (uint16_t)(words[e >> 1] >> (e & 1u ? 16 : 0));
+                for (uint32_t it = 0; it < kPieces / 2u; ++it, at += step) store16(at, w[it]);
+            } else {
+#pragma unroll 1
+                for (uint32_t it = 0; it < kPieces / 2u; ++it) {
+                    const uint32_t m = row + it * (64u / kPieces);
+                    const uint4 w = *place(r0 + it * (64u / kPieces), piece);
+                    uint8_t* at = static_cast<uint8_t*>(out) + (m * pitch + n) * (kHalf16 ? 2u : 4u);
+                    if (m >= a.M || n >= columns) continue;
+                    if (kWide) {
+                        store4<kHalf16>(at, f32x4{__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)}, columns - n, add);
+                    } else if (n + 8u <= columns) {
+                        store16(at, w);
+                    } else {
+                        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (uint32_t e = 0; e < 7u; ++e)
+                            if (n + e < columns) reinterpret_cast<uint16_t*>(at)[e] = (uint16_t)(words[e >> 1] >> (e & 1u ? 16 : 0));
+                    }
                 }
+                __builtin_amdgcn_s_waitcnt(0x0F70);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
     };
-    if (a.share < blocks) {
-        const uint64_t pitch = fp8_part_pitch(a.N);
-        emit(std::true_type{}, std::false_type{}, a.workspace + blockIdx.y * a.M * pitch, pitch, (uint32_t)pitch, false);
-    } else if constexpr (EXACT) {
-        emit(std::true_type{}, std::false_type{}, a.c, a.ldc, a.N, a.accumulate);
-    } else if (a.accumulate) {   // (the old value is added before the only rounding)
-        emit(std::true_type{}, std::true_type{}, a.c, a.ldc, a.N, true);
-    } else {
-        emit(std::false_type{}, std::true_type{}, a.c, a.ldc, a.N, false);
+    go_to(blockIdx.x);
+    begin();
+    __builtin_amdgcn_s_waitcnt(all_but(kWalks ? 0u : 4u * MF) | 0xF70u);
+    for (uint32_t tile = blockIdx.x;;) {
+        float zero;
+        asm volatile("v_mov_b32 %0, 0" : "=v"(zero));   // (else sixteen zeros are kept for the next tile)
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = zero;
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < MF; ++i) sa[i] >>= 8u * (first & 3u);
+#pragma unroll
+        for (int j = 0; j < NF; ++j) sb[j] >>= 8u * (first & 3u);
+        read(0, 0, fa0, fb0);
+        if constexpr (EXACT)
+#pragma unroll
+            for (uint32_t f = 0; f < MF + NF; ++f) widen(0, f, 0, fa0, fb0, sa, sb);
+        __builtin_amdgcn_sched_barrier(0);
+        uint32_t k = 0;
+        for (; k + 4u < steps; k += 5u) {
+            step(std::integral_constant<uint32_t, 0>{}, k);
+            step(std::integral_constant<uint32_t, 1>{}, k + 1u);
+            step(std::integral_constant<uint32_t, 2>{}, k + 2u);
+            step(std::integral_constant<uint32_t, 3>{}, k + 3u);
+            step(std::integral_constant<uint32_t, 4>{}, k + 4u);
+        }
+        if (k < steps) step(std::integral_constant<uint32_t, 0>{}, k);
+        if (k + 1u < steps) step(std::integral_constant<uint32_t, 1>{}, k + 1u);
+        if (k + 2u < steps) step(std::integral_constant<uint32_t, 2>{}, k + 2u);
+        if (k + 3u < steps) step(std::integral_constant<uint32_t, 3>{}, k + 3u);
+        __builtin_amdgcn_s_waitcnt(0x0070);   // (what was fetched behind the last step, and read)
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        up_to_here();
+        const uint32_t m = m0, n = n0;
+        tile += gridDim.x;
+        const bool more = kWalks && tile < tiles_m * tiles_n;
+        if (more) {
+            go_to(tile);
+            begin();
+        }
+        // Whole tiles leave in a known number of stores, which are still on their way when the next tile begins: only its first two steps,
+        // fetched before them, are waited for.
+        using yes = std::true_type;
+        using no = std::false_type;
+        const bool whole = m + BM <= a.M && n + BN <= a.N && !a.accumulate;
+        if (!kWalks && a.share < blocks) {   // (the larger tiles are not divided)
+            const uint64_t pitch = fp8_part_pitch(a.N);
+            emit(yes{}, no{}, whole, m, n, a.workspace + blockIdx.y * a.M * pitch, pitch, (uint32_t)pitch, false);
+            break;
+        } else if (EXACT) {
+            emit(yes{}, no{}, whole, m, n, a.c, a.ldc, a.N, a.accumulate);
+            if (!more) break;
+            __builtin_amdgcn_s_waitcnt(all_but(4u * MF * NF) | 0xF70u);
+        } else if (a.accumulate) {   // (the old value is added before the only rounding)
+            emit(yes{}, yes{}, false, m, n, a.c, a.ldc, a.N, true);
+            if (!more) break;
+        } else {
+            emit(no{}, yes{}, whole, m, n, a.c, a.ldc, a.N, false);
+            if (!more) break;
+            __builtin_amdgcn_s_waitcnt(all_but(2u * MF * NF) | 0xF70u);
+        }
     }
 }
 
@@ -351,8 +406,11 @@ __global__ __launch_bounds__(256) void zero_matrix_kernel(Fp8MatmulArgs a) {
 // How a product is done, by its sizes alone (an order of additions may depend on nothing else).  Measured on the device:
 //  - up to 16 rows: direct, unless there are 24576 rows of B or more (one row, 2048 along k: 8192 rows of B 7.5 us direct and
 //    10.6 us tiled, 50257 rows 41 and 21 us);
-//  - tiles of 256 x 256 from 160 of them on, three out of five compute units (2048 x 4096 x 2048, 128 tiles: 28 us, and 20 us in
-//    tiles of 128 x 128; 3000 x 4096 x 2048, 192 tiles: 31 and 30 us; 4096^3, 256 tiles: 55 and 67 us);
+//  - tiles of 256 x 256 where they are expected to be shorter: 256 of them run at a time, 512 of 128 x 128, two on a compute unit
+//    and 1.4 times as long for their size (bf16 results, which wait for memory) or 1.06 times (fp32), the last of them less.
+//    Measured, in us with 256 and 128, bf16 and fp32: 2048 x 4096 x 2048 26 and 19, 46 and 30; 3000 x 4096 x 2048 29 and 29, 53 and 45;
+//    4096 x 4096 x 2048 31 and 37, 57 and 58; 4608 x 4096 x 2048 48 and 43, 90 and 67; 7168 x 4096 x 2048 54 and 61, 104 and 96;
+//    1024 x 50304 x 1024 66 and 73, 119 and 118; 16384 x 8192 x 8192 705 and 905; 8192^3 fp32 690 and 740;
 //  - short products of few tiles of 128 x 128: direct, tiles of 64 x 64 (777 x 520 x 1000, 35 tiles: 8.1 and 12 us;
 //    1024^3, 64 tiles: 8.0 and 6.7 us; 64 x 2048 x 2048, 16 tiles of 16 blocks each: 11.5 and 8.8 us);
 //  - tiles of 128 x 128 otherwise, the blocks along k divided among workgroups where that is expected to be
@@ -363,7 +421,7 @@ struct Plan {
     uint32_t tile;      // of the tiled kernel: 256 or 128; of the direct one: 64 or 16 (rows)
     uint32_t parts;     // among which the blocks along k are divided
 };
-static Plan plan_for(uint64_t M, uint64_t N, uint64_t K) {
+static Plan plan_for(uint64_t M, uint64_t N, uint64_t K, bool bf16) {
     auto tiles = [&](uint64_t rows, uint64_t cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
     const uint64_t steps = (K + kStep - 1) / kStep;
     if (M <= kFp8FewRows && N < 24576u) {
@@ -371,8 +429,8 @@ static Plan plan_for(uint64_t M, uint64_t N, uint64_t K) {
         parts = parts < steps / 16u ? parts : steps / 16u;
         return {16u, (uint32_t)(parts > 1u ? parts : 1u)};
     }
-    if (tiles(256, 256) >= 160u) return {256u, 1u};
     const uint64_t count = tiles(128, 128);
+    if (4.0 * ((tiles(256, 256) + kUnits - 1u) / kUnits) < (bf16 ? 2.8 : 2.12) * (count > 512u ? count / 512.0 : 1.0)) return {256u, 1u};
     if (count < 48u && tiles(64, 64) >= 40u && steps <= 12u) return {64u, 1u};
     Plan best{128u, 1u};
     double least = 0.45 * steps;
@@ -386,15 +444,15 @@ static Plan plan_for(uint64_t M, uint64_t N, uint64_t K) {
     return best;
 }
 
-bool fp8_product_is_direct(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K).tile == 16u; }
+bool fp8_product_is_direct(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K, true).tile == 16u; }
 
 uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
     if (M == 0 || N == 0 || K == 0) return 0;
-    const Plan p = plan_for(M, N, K);
+    const Plan p = plan_for(M, N, K, true);   // (the two types of results differ in tiles only where no plan has parts)
     return p.parts > 1u ? p.parts * M * fp8_part_pitch(N) * sizeof(float) : 0;
 }
 
-uint32_t fp8_direct_parts(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K).parts; }
+uint32_t fp8_direct_parts(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K, true).parts; }
 
 hipError_t launch_fp8_matmul(const Fp8MatmulArgs& args, hipStream_t stream) {
     Fp8MatmulArgs a = args;
@@ -404,7 +462,7 @@ hipError_t launch_fp8_matmul(const Fp8MatmulArgs& args, hipStream_t stream) {
         zero_matrix_kernel<<<(uint32_t)(blocks < 4096u ? blocks : 4096u), 256, 0, stream>>>(a);
         return hipGetLastError();
     }
-    const Plan plan = plan_for(a.M, a.N, a.K);
+    const Plan plan = plan_for(a.M, a.N, a.K, a.out_bf16);
     if (plan.tile < 128u) {
         Fp8DirectArgs direct{};
         static_cast<Fp8MatmulArgs&>(direct) = a;
@@ -416,7 +474,9 @@ hipError_t launch_fp8_matmul(const Fp8MatmulArgs& args, hipStream_t stream) {
     const uint32_t tm = (uint32_t)tiles_m, tn = (uint32_t)tiles_n;
     a.share = (blocks + plan.parts - 1u) / plan.parts;
     const uint32_t parts = (blocks + a.share - 1u) / a.share;
-    const dim3 grid(tm * tn, parts);
+    // (tiles of 256 x 256 are walked by a workgroup on each compute unit)
+    const uint64_t workgroups = plan.tile == 256u && tiles_m * tiles_n > kUnits ? kUnits : tiles_m * tiles_n;
+    const dim3 grid((uint32_t)workgroups, parts);
     auto go = [&](auto FA, auto FB, auto EXACT) {
         constexpr int A = decltype(FA)::value, B = decltype(FB)::value;
         constexpr bool E = decltype(EXACT)::value;
