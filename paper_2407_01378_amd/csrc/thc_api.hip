@@ -1213,7 +1213,7 @@ int thc_fp8_matmul(const uint8_t* a, const uint8_t* a_scales, int a_format, cons
 }
 
 // Few rows are quantized by the workgroups of the product themselves.
-static bool linear_in_one_launch(uint64_t M, uint64_t N, uint64_t K) { return K != 0 && thc::fp8_product_is_direct(M, N, K); }
+static bool linear_in_one_launch(uint64_t M, uint64_t N, uint64_t K) { return K != 0 && M <= thc::kFp8FewRows && thc::fp8_rows_are_few(M, N, K); }
 
 // The workspace of thc_fp8_linear: the codes of x, its scales, the product's own workspace.
 uint64_t thc_fp8_linear_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {

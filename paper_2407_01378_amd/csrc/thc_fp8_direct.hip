@@ -218,10 +218,10 @@ hipError_t with_types(const Fp8MatmulArgs& a, F&& go) {
 
 hipError_t launch_fp8_direct(const Fp8DirectArgs& args, hipStream_t stream) {
     Fp8DirectArgs a = args;
-    const bool few = fp8_product_is_direct(a.M, a.N, a.K);
-    const uint32_t rows = few ? 16u : 64u, wanted = fp8_direct_parts(a.M, a.N, a.K), steps = (a.K + 127u) / 128u;
-    const uint32_t tiles_m = (a.M + rows - 1u) / rows, tiles_n = (a.N + rows - 1u) / rows;
-    if (steps == 0u || (uint64_t)tiles_m * tiles_n > (1u << 22) || (!few && a.source != 0u)) return hipErrorInvalidValue;
+    const bool few = fp8_rows_are_few(a.M, a.N, a.K);
+    const uint32_t cols = few ? 16u : 64u, rows = few && a.M > 16u ? 32u : cols, wanted = fp8_direct_parts(a.M, a.N, a.K), steps = (a.K + 127u) / 128u;
+    const uint32_t tiles_m = (a.M + rows - 1u) / rows, tiles_n = (a.N + cols - 1u) / cols;
+    if (steps == 0u || (uint64_t)tiles_m * tiles_n > (1u << 22) || (a.source != 0u && !(few && rows == 16u))) return hipErrorInvalidValue;
     a.share = (steps + wanted - 1u) / wanted;
     const uint32_t parts = (steps + a.share - 1u) / a.share;
     const dim3 grid(tiles_m * tiles_n, parts);
@@ -229,9 +229,11 @@ hipError_t launch_fp8_direct(const Fp8DirectArgs& args, hipStream_t stream) {
         constexpr int A = decltype(FA)::value, B = decltype(FB)::value;
         constexpr bool E = decltype(EXACT)::value;
         auto go = [&](auto S) {
-            fp8_direct_kernel<A, B, E, decltype(S)::value, 1, 1, kFewWaves><<<grid, 64 * kFewWaves, 0, stream>>>(a, tiles_m, tiles_n);
+            constexpr int kSource = decltype(S)::value;
+            fp8_direct_kernel<A, B, E, kSource, 1, 1, kFewWaves><<<grid, 64 * kFewWaves, 0, stream>>>(a, tiles_m, tiles_n);
         };
         if (!few) fp8_direct_kernel<A, B, E, 0, 4, 4, 4><<<grid, 256, 0, stream>>>(a, tiles_m, tiles_n);
+        else if (rows == 32u) fp8_direct_kernel<A, B, E, 0, 2, 1, kFewWaves><<<grid, 64 * kFewWaves, 0, stream>>>(a, tiles_m, tiles_n);
         else if (a.source == 0u) go(I0{});
         else if (a.source == 1u) go(I1{});
         else go(I2{});

@@ -404,8 +404,9 @@ __global__ __launch_bounds__(256) void zero_matrix_kernel(Fp8MatmulArgs a) {
 }  // namespace
 
 // How a product is done, by its sizes alone (an order of additions may depend on nothing else).  Measured on the device:
-//  - up to 16 rows: direct, unless there are 24576 rows of B or more (one row, 2048 along k: 8192 rows of B 7.5 us direct and
-//    10.6 us tiled, 50257 rows 41 and 21 us);
+//  - up to 16 rows: direct, unless there are 24576 rows of B or more (2048 along k: one row and 8192 rows of B 7.5 us direct and
+//    10.6 us tiled; 16 rows and 16384 rows of B 11.4 and 12.7 us, 24576 16 and 13 us, 50257 34 and 23 us);
+//    up to 32 rows, for 4096 rows of B or fewer (32 rows: 2048 x 2048 5.8 and 9.1 us, 2048 x 8192 11 and 14 us, 8192 x 2048 11 and 10 us);
 //  - tiles of 256 x 256 where they are expected to be shorter: 256 of them run at a time, 512 of 128 x 128, two on a compute unit
 //    and 1.4 times as long for their size (bf16 results, which wait for memory) or 1.06 times (fp32), the last of them less.
 //    Measured, in us with 256 and 128, bf16 and fp32: 2048 x 4096 x 2048 26 and 19, 46 and 30; 3000 x 4096 x 2048 29 and 29, 53 and 45;
@@ -418,14 +419,14 @@ __global__ __launch_bounds__(256) void zero_matrix_kernel(Fp8MatmulArgs a) {
 //    (1024 x 1024 x 16384: 59 us undivided, 41, 29 and 31 us in 2, 4 and 8 parts; 512 x 2048 x 2048: 11, 15 and 20 us in 1, 2
 //    and 4 parts).
 struct Plan {
-    uint32_t tile;      // of the tiled kernel: 256 or 128; of the direct one: 64 or 16 (rows)
+    uint32_t tile;      // of the tiled kernel: 256 or 128; of the direct one: 64, or 16 (few rows: all of A, 16 of B)
     uint32_t parts;     // among which the blocks along k are divided
 };
 static Plan plan_for(uint64_t M, uint64_t N, uint64_t K, bool bf16) {
     auto tiles = [&](uint64_t rows, uint64_t cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
     const uint64_t steps = (K + kStep - 1) / kStep;
-    if (M <= kFp8FewRows && N < 24576u) {
-        uint64_t parts = 256u / tiles(16, 16);   // (no part shorter than two blocks for each of 8 waves)
+    if ((M <= kFp8FewRows && N < 24576u) || (M <= 2u * kFp8FewRows && N <= 4096u)) {
+        uint64_t parts = 256u / tiles(M > kFp8FewRows ? 2u * kFp8FewRows : kFp8FewRows, 16);   // (no part shorter than two blocks for each of 8 waves)
         parts = parts < steps / 16u ? parts : steps / 16u;
         return {16u, (uint32_t)(parts > 1u ? parts : 1u)};
     }
@@ -444,7 +445,7 @@ static Plan plan_for(uint64_t M, uint64_t N, uint64_t K, bool bf16) {
     return best;
 }
 
-bool fp8_product_is_direct(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K, true).tile == 16u; }
+bool fp8_rows_are_few(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K, true).tile == 16u; }
 
 uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
     if (M == 0 || N == 0 || K == 0) return 0;

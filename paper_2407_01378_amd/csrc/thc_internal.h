@@ -269,7 +269,7 @@ struct Fp8DirectArgs : Fp8MatmulArgs {
     uint64_t ldx;
     uint32_t source;
 };
-bool fp8_product_is_direct(uint64_t M, uint64_t N, uint64_t K);   // few rows, and this is how thc_fp8_matmul does it
+bool fp8_rows_are_few(uint64_t M, uint64_t N, uint64_t K);   // and launch_fp8_direct is how thc_fp8_matmul does them
 uint32_t fp8_direct_parts(uint64_t M, uint64_t N, uint64_t K);
 hipError_t launch_fp8_direct(const Fp8DirectArgs& a, hipStream_t stream);
 
