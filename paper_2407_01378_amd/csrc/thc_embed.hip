@@ -370,30 +370,47 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
     float sum[8] = {};
     float* part = s.parts + (uint64_t)p * s.pitch + d;
     auto keep = [&](float* to) { Row8<false>::store(to, sum); };
-    constexpr uint32_t kAhead = 8;
-    for (uint32_t i = begin; i < end; i += kAhead) {
-        uint32_t k[kAhead];
-        float v[kAhead][8];
+    // Rows are loaded several at a time, those of tokens outside the table at the border too (they are rows of grad_out like the
+    // others); keys and places a step ahead.
+    constexpr uint32_t kAhead = IN ? 16 : 8;
+    uint32_t k[kAhead], place[kAhead];
+    auto look = [&](uint32_t i) {
 #pragma unroll
         for (uint32_t q = 0; q < kAhead; ++q) {
             const uint32_t j = i + q < end ? i + q : end - 1u;
             k[q] = s.keys[j];
-            if (k[q] < a.vocab) load_row<IN>(a.in, (uint64_t)s.places[j] * a.ld_in + d, valid, v[q]);
+            place[q] = s.places[j];
         }
+    };
+    look(begin);
+    for (uint32_t i = begin; i < end; i += kAhead) {
+        Row8<IN> v[kAhead];
+        uint32_t now[kAhead];
+        if (k[0] < a.vocab) {
+            if (valid >= 8u) {
+#pragma unroll
+                for (uint32_t q = 0; q < kAhead; ++q)
+                    v[q].load(static_cast<const uint8_t*>(a.in) + ((uint64_t)place[q] * a.ld_in + d) * (IN ? 2u : 4u));
+            } else {
+#pragma unroll
+                for (uint32_t q = 0; q < kAhead; ++q) v[q].load_some(a.in, (uint64_t)place[q] * a.ld_in + d, valid);
+            }
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kAhead; ++q) now[q] = k[q];
+        if (i + kAhead < end) look(i + kAhead);
 #pragma unroll
         for (uint32_t q = 0; q < kAhead; ++q) {
             if (i + q >= end) continue;
-            if (k[q] != key) {
+            if (now[q] != key) {
                 if (open) keep(part);
                 else finish_row<OUT>(a, key, d, valid, sum);
-                key = k[q];
+                key = now[q];
                 open = false;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
             }
-            if (key < a.vocab)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += v[q][e];
+            if (key < a.vocab) v[q].add_to(sum);
         }
         if (key >= a.vocab) return;   // (nothing but such follows)
     }
@@ -415,23 +432,28 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, SumAr
     if (first_key == key && begin != 0u && before == key) return;          // it has begun before
     float sum[8];
     load_row<false>(s.parts, ((uint64_t)s.pieces + p) * s.pitch + d, 8u, sum);
+    // pieces that begin with the run, 16 at a time; their parts are loaded where there are such pieces (most runs end in the next one)
+    constexpr uint32_t kAhead = 16;
+    uint32_t first[kAhead];
+    auto look = [&](uint32_t q) {
+#pragma unroll
+        for (uint32_t r = 0; r < kAhead; ++r) first[r] = s.keys[(q + r < s.pieces ? q + r : s.pieces - 1u) * s.piece];
+    };
+    look(p + 1u);
     bool more = true;
-    for (uint32_t q = p + 1u; more && q < s.pieces; q += 8u) {   // pieces that begin with the run, 8 at a time
-        float v[8][8];
-        uint32_t first[8];
+    for (uint32_t q = p + 1u; more && q < s.pieces; q += kAhead) {
+        Row8<false> v[kAhead];
+        bool in[kAhead];
 #pragma unroll
-        for (uint32_t r = 0; r < 8u; ++r) {
-            const uint32_t i = q + r < s.pieces ? q + r : s.pieces - 1u;
-            first[r] = s.keys[i * s.piece];
-            load_row<false>(s.parts, (uint64_t)i * s.pitch + d, 8u, v[r]);
-        }
-#pragma unroll
-        for (uint32_t r = 0; r < 8u; ++r) {
+        for (uint32_t r = 0; r < kAhead; ++r) {
             more = more && q + r < s.pieces && first[r] == key;
-            if (more)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += v[r][e];
+            in[r] = more;
+            if (more) v[r].load(s.parts + (uint64_t)(q + r) * s.pitch + d);
         }
+        if (more) look(q + kAhead);
+#pragma unroll
+        for (uint32_t r = 0; r < kAhead; ++r)
+            if (in[r]) v[r].add_to(sum);
     }
     finish_row<OUT>(a, key, d, a.dim - d, sum);
 }

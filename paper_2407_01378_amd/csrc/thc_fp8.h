@@ -143,6 +143,18 @@ struct Row8 {
 #pragma unroll
         for (int i = 0; i < (BF16 ? 1 : 2); ++i) w[i] = load16(static_cast<const uint4*>(c) + i);
     }
+    // the first `valid` (fewer than 8) of them, zeros behind
+    __device__ __forceinline__ void load_some(const void* c, uint64_t at, uint32_t valid) {
+        uint32_t x[8];
+#pragma unroll
+        for (uint32_t e = 0; e < 8u; ++e) x[e] = e >= valid ? 0u : BF16 ? static_cast<const uint16_t*>(c)[at + e] : static_cast<const uint32_t*>(c)[at + e];
+        if (BF16) {
+            w[0] = make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+        } else {
+            w[0] = make_uint4(x[0], x[1], x[2], x[3]);
+            w[BF16 ? 0 : 1] = make_uint4(x[4], x[5], x[6], x[7]);
+        }
+    }
     __device__ __forceinline__ void add_to(float (&v)[8]) const {
         const uint32_t x[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[BF16 ? 0 : 1].x, w[BF16 ? 0 : 1].y, w[BF16 ? 0 : 1].z, w[BF16 ? 0 : 1].w};
 #pragma unroll
