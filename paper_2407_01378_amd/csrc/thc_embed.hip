@@ -6,7 +6,12 @@
 // length, and a group of lanes adds the rows of a piece, run by run of equal tokens: however often a token occurs,
 // the work is divided evenly, and every sum has one order.  A run inside a piece is written directly; of a run that
 // crosses a piece's border the piece keeps its part, and a last launch adds the parts.  Rows of the table whose token does not occur are
-// zeroed by further workgroups of the summing launch.  Where the whole gradient is written, that write is what bounds it.
+// zeroed by further workgroups of the sorting and the summing launches.
+//
+// What bounds it: memory.  Lookup: 8192 rows of 2048 bf16 10.2 us, 67 MB, 6.6 TB/s (rows that occur often come from the caches).  Gradient: the
+// write of the whole table, 4.0 TB/s while the tokens are sorted beside it (8192 tokens, 50257 x 1024 to fp32: 65 us, 223 MB); then the way through
+// memory that a piece's keys, its rows and the parts of the longest run take one after the other (the sums of 8192 x 1024 bf16 by
+// themselves 15 us, the last launch 7 us).
 #include "thc_fp8.h"
 #include "thc_internal.h"
 

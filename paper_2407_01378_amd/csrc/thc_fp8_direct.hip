@@ -2,11 +2,15 @@
 // once, and products of too few tiles for the tiled kernel; and y = Q(x) B^T in one launch for few rows.
 //
 // A workgroup takes 16 MF rows of A and 16 NF rows of B.  Its waves take the blocks of 128 along k in turn, with operands
-// straight from memory in the layout of the 16 x 16 matrix instruction (four lanes
-// hold a row's 128 codes, 16 of each 64 neighbouring ones a lane), several blocks in flight; their sums are added in their order through LDS.  Where the tiles
-// are too few for the device the blocks along k are also divided among workgroups, whose sums a second launch adds.
-// With x in fp32 or bf16 a lane quantizes the 32 values it needs itself: every workgroup quantizes its part of x, which for few
+// straight from memory in the layout of the 16 x 16 matrix instruction (four lanes hold a row's 128 codes, 16 of each 64
+// neighbouring ones a lane), several blocks in flight; their sums are added in their order through LDS.  Where the tiles are too few
+// for the device the blocks along k are also divided among workgroups, whose sums a second launch adds.
+// With x in fp32 or bf16 a lane quantizes the 32 values it needs itself: every workgroup quantizes its part of x, which for up to 16
 // rows costs less than a launch.
+//
+// What bounds it: the latency of memory, then its bandwidth.  One token, 2048 along k, 8192 rows of weights: 6.1 us for 16.8 MB, 2.7 TB/s (an
+// empty launch takes 2 us of it); 16 rows and 16384 rows of weights 11.4 us, 2.9 TB/s.  8 waves to a workgroup:
+// the token's product in 4, 8 and 16 waves took 6.9, 6.4 and 8.0 us, from codes 5.4, 5.5 and 7.3 us.
 #include "thc_fp8.h"
 #include "thc_internal.h"
 

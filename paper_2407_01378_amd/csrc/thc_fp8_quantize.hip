@@ -4,7 +4,9 @@
 // magnitude is a maximum over 16 lanes (inside the vector ALU) and a column's a maximum over the workgroup (through
 // LDS).  Both forms, along the rows and along the columns, come from one read of x; the codes of the
 // transposed form pass through LDS so that every store is a whole piece of a row.
-// What bounds it: memory, 2 or 4 bytes read and 1 written per value and form.
+// What bounds it: memory, 2 or 4 bytes read and 1 written per value and form.  Measured: 8192 x 8192 bf16, both forms, 61 us and
+// 8192 x 2048 fp32 by tiles, both forms, 23 us, 4.4 TB/s each (a 4 GiB copy reaches 4.7); back from codes 14.5 us (8192 x 2048 to fp32).  A
+// small matrix, of fewer tiles than compute units, takes 6 us whatever its size: one tile's way through memory and LDS.
 #include "thc_device.h"
 #include "thc_fp8.h"
 #include "thc_internal.h"
@@ -206,7 +208,8 @@ __global__ __launch_bounds__(kThreads) void fp8_quantize_kernel(Fp8QuantizeArgs 
     }
 }
 
-// Along the rows only: 16 lanes take a block, a wave 4 neighbouring blocks of a row, which share their scale word.
+// Along the rows only: 16 lanes take a block, a wave 4 neighbouring blocks of a row, which share their scale word.  (No tile has to
+// come together, so a few rows are spread over the device: 24 x 8192 bf16 2.9 us.)
 template <bool BF16, bool E5M2>
 __global__ __launch_bounds__(kThreads) void fp8_quantize_rows_kernel(Fp8QuantizeArgs a, uint32_t groups, uint64_t total) {
     const uint32_t lane = threadIdx.x & 63u, cg = lane & 15u, blocks = (a.cols + 127u) / 128u;
