@@ -1,5 +1,5 @@
 // C = A B^T of two 8-bit matrices straight from memory: few rows (tokens of a few sequences), where the time is that of reading B
-// once, and products of too few tiles for the tiled kernel; and y = Q(x) B^T in one launch for few rows.
+// once, and fp32 products of too few tiles for the tiled kernel; and y = Q(x) B^T in one launch for few rows.
 //
 // A workgroup takes 16 MF rows of A and 16 NF rows of B.  Its waves take the blocks of 128 along k in turn, with operands
 // straight from memory in the layout of the 16 x 16 matrix instruction (four lanes hold a row's 128 codes, 16 of each 64
@@ -223,7 +223,7 @@ hipError_t with_types(const Fp8MatmulArgs& a, F&& go) {
 hipError_t launch_fp8_direct(const Fp8DirectArgs& args, hipStream_t stream) {
     Fp8DirectArgs a = args;
     const bool few = fp8_rows_are_few(a.M, a.N, a.K);
-    const uint32_t cols = few ? 16u : 64u, rows = few && a.M > 16u ? 32u : cols, wanted = fp8_direct_parts(a.M, a.N, a.K), steps = (a.K + 127u) / 128u;
+    const uint32_t cols = few ? 16u : 64u, rows = few && a.M > 16u ? 32u : cols, wanted = few ? fp8_few_rows_parts(a.M, a.N, a.K) : 1u, steps = (a.K + 127u) / 128u;
     const uint32_t tiles_m = (a.M + rows - 1u) / rows, tiles_n = (a.N + cols - 1u) / cols;
     if (steps == 0u || (uint64_t)tiles_m * tiles_n > (1u << 22) || (a.source != 0u && !(few && rows == 16u))) return hipErrorInvalidValue;
     a.share = (steps + wanted - 1u) / wanted;
@@ -236,8 +236,10 @@ hipError_t launch_fp8_direct(const Fp8DirectArgs& args, hipStream_t stream) {
             constexpr int kSource = decltype(S)::value;
             fp8_direct_kernel<A, B, E, kSource, 1, 1, kFewWaves><<<grid, 64 * kFewWaves, 0, stream>>>(a, tiles_m, tiles_n);
         };
-        if (!few) fp8_direct_kernel<A, B, E, 0, 4, 4, 4><<<grid, 256, 0, stream>>>(a, tiles_m, tiles_n);
-        else if (rows == 32u) fp8_direct_kernel<A, B, E, 0, 2, 1, kFewWaves><<<grid, 64 * kFewWaves, 0, stream>>>(a, tiles_m, tiles_n);
+        if (!few) {
+            if constexpr (E) fp8_direct_kernel<A, B, true, 0, 4, 4, 4><<<grid, 256, 0, stream>>>(a, tiles_m, tiles_n);
+            else return hipErrorInvalidValue;   // (no plan)
+        } else if (rows == 32u) fp8_direct_kernel<A, B, E, 0, 2, 1, kFewWaves><<<grid, 64 * kFewWaves, 0, stream>>>(a, tiles_m, tiles_n);
         else if (a.source == 0u) go(I0{});
         else if (a.source == 1u) go(I1{});
         else go(I2{});

@@ -12,6 +12,8 @@
 // library product in bf16 1.5 to 1.6), busy 73 %.  Why 256 x 256: each step brings 64 KB to a compute unit for 1000 cycles of products
 // (8192 x 2048 x 8192 to bf16 97 us, 120 in tiles of 128 x 128).  A step is not read until it lies in LDS whole; with one step ahead instead of two
 // to two and a half the loop waited for memory.  No bank of LDS is asked twice at a time.
+#include <initializer_list>
+
 #include "thc_fp8.h"
 #include "thc_internal.h"
 
@@ -421,8 +423,8 @@ __global__ __launch_bounds__(256) void zero_matrix_kernel(Fp8MatmulArgs a) {
 //    Measured, in us with 256 and 128, bf16 and fp32: 2048 x 4096 x 2048 26 and 19, 46 and 30; 3000 x 4096 x 2048 29 and 29, 53 and 45;
 //    4096 x 4096 x 2048 31 and 37, 57 and 58; 4608 x 4096 x 2048 48 and 43, 90 and 67; 7168 x 4096 x 2048 54 and 61, 104 and 96;
 //    1024 x 50304 x 1024 66 and 73, 119 and 118; 16384 x 8192 x 8192 705 and 905; 8192^3 fp32 690 and 740;
-//  - short products of few tiles of 128 x 128: direct, tiles of 64 x 64 (777 x 520 x 1000, 35 tiles: 8.1 and 12 us;
-//    1024^3, 64 tiles: 8.0 and 6.7 us; 64 x 2048 x 2048, 16 tiles of 16 blocks each: 11.5 and 8.8 us);
+//  - short fp32 products of few tiles of 128 x 128: direct, tiles of 64 x 64 (777 x 520 x 1000, 35 tiles: 8.4 and 9.4 us, to bf16
+//    8.0 and 6.8; 512 x 512 x 1536 10.4 and 11.0 us, to bf16 9.8 and 7.6);
 //  - tiles of 128 x 128 otherwise, the blocks along k divided among workgroups where that is expected to be
 //    shorter: a block takes such a tile 0.45 us, a second launch 2 us, and the parts' sums pass memory twice at about 3 TB/s
 //    (1024 x 1024 x 16384: 59 us undivided, 41, 29 and 31 us in 2, 4 and 8 parts; 512 x 2048 x 2048: 11, 15 and 20 us in 1, 2
@@ -441,7 +443,7 @@ static Plan plan_for(uint64_t M, uint64_t N, uint64_t K, bool bf16) {
     }
     const uint64_t count = tiles(128, 128);
     if (4.0 * ((tiles(256, 256) + kUnits - 1u) / kUnits) < (bf16 ? 2.8 : 2.12) * (count > 512u ? count / 512.0 : 1.0)) return {256u, 1u};
-    if (count < 48u && tiles(64, 64) >= 40u && steps <= 12u) return {64u, 1u};
+    if (!bf16 && count < 48u && tiles(64, 64) >= 40u && steps <= 12u) return {64u, 1u};
     Plan best{128u, 1u};
     double least = 0.45 * steps;
     for (uint32_t parts = 2; parts * count <= 512u && parts * 4u <= steps; parts *= 2u) {
@@ -458,11 +460,16 @@ bool fp8_rows_are_few(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N
 
 uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
     if (M == 0 || N == 0 || K == 0) return 0;
-    const Plan p = plan_for(M, N, K, true);   // (the two types of results differ in tiles only where no plan has parts)
-    return p.parts > 1u ? p.parts * M * fp8_part_pitch(N) * sizeof(float) : 0;
+    uint64_t bytes = 0;   // enough for either type of results
+    for (const bool bf16 : {false, true}) {
+        const Plan p = plan_for(M, N, K, bf16);
+        const uint64_t need = p.parts > 1u ? p.parts * M * fp8_part_pitch(N) * sizeof(float) : 0;
+        bytes = need > bytes ? need : bytes;
+    }
+    return bytes;
 }
 
-uint32_t fp8_direct_parts(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K, true).parts; }
+uint32_t fp8_few_rows_parts(uint64_t M, uint64_t N, uint64_t K) { return plan_for(M, N, K, true).parts; }
 
 hipError_t launch_fp8_matmul(const Fp8MatmulArgs& args, hipStream_t stream) {
     Fp8MatmulArgs a = args;

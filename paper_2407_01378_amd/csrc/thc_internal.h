@@ -261,8 +261,8 @@ uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
 hipError_t launch_fp8_matmul(const Fp8MatmulArgs& a, hipStream_t stream);
 // The sum of the parts in a.workspace, in their order, to a.c.
 hipError_t launch_fp8_join(const Fp8MatmulArgs& a, uint32_t parts, hipStream_t stream);
-// Operands straight from memory, K > 0: tiles of 64 x 64, or, up to kFp8FewRows rows, 16 rows of B to a workgroup; there A is
-// given as codes (source 0) or as values to be quantized on the way (1 = bf16, 2 = fp32).
+// Operands straight from memory, K > 0: tiles of 64 x 64 (fp32 results), or, for few rows, 16 rows of B to a workgroup; up to
+// kFp8FewRows rows A is given as codes (source 0) or as values to be quantized on the way (1 = bf16, 2 = fp32).
 constexpr uint32_t kFp8FewRows = 16;
 struct Fp8DirectArgs : Fp8MatmulArgs {
     const void* x;
@@ -270,7 +270,7 @@ struct Fp8DirectArgs : Fp8MatmulArgs {
     uint32_t source;
 };
 bool fp8_rows_are_few(uint64_t M, uint64_t N, uint64_t K);   // and launch_fp8_direct is how thc_fp8_matmul does them
-uint32_t fp8_direct_parts(uint64_t M, uint64_t N, uint64_t K);
+uint32_t fp8_few_rows_parts(uint64_t M, uint64_t N, uint64_t K);
 hipError_t launch_fp8_direct(const Fp8DirectArgs& a, hipStream_t stream);
 
 // ---- embedding (thc_embed.hip) -----------------------------------------------------------------

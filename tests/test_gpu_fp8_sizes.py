@@ -33,7 +33,7 @@ def _operand(rows, cols, fmt, seed):
     (16, 24575, 260), (16, 24576, 260), (17, 24575, 1100), (1, 50257, 900), (3, 70001, 128),    # few rows
     (32, 4096, 300), (33, 4096, 300), (17, 4097, 5000), (32, 33, 6000), (29, 2048, 8192),
     (16, 4096, 4096), (17, 300, 8000), (128, 128, 70000), (40, 5000, 9000),              # long sums
-    (640, 640, 1536), (639, 641, 1537), (900, 1000, 1664)])
+    (640, 640, 1536), (639, 641, 1537), (900, 1000, 1664), (4082, 18, 1443), (2722, 25, 1472), (777, 520, 1000)])
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
 def test_exact(M, N, K, out):
     a, b = _operand(M, K, thc.THC_E5M2, 1), _operand(N, K, thc.THC_E4M3, 2)
