@@ -235,65 +235,37 @@ __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(EmbedArgs a, Sor
     }
 }
 
-// Up to kFew tokens: the whole sort in one workgroup, in LDS, 8 bits at a time.
-constexpr uint32_t kFew = 4096, kFewThreads = 1024;
-__global__ __launch_bounds__(kFewThreads) void sort_few_kernel(EmbedArgs a, uint32_t* keys_out, uint32_t* places_out, uint32_t key_bits, ZeroShare z) {
-    if (zeroes(a, z, 1u)) return;
-    constexpr uint32_t kWaves = kFewThreads / 64u;
-    __shared__ uint32_t s_key[2][kFew], s_place[2][kFew], s_next[kWaves][256], s_wave[kWaves];
-    const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6;
-    // a wave has a run of whole groups of 64
-    const uint32_t groups = (a.count + 63u) / 64u, share = (groups + kWaves - 1u) / kWaves * 64u;
-    const uint32_t from = wave * share < a.count ? wave * share : a.count, to = a.count - from < share ? a.count : from + share;
-    for (uint32_t i = t; i < a.count; i += kFewThreads) {
-        s_key[0][i] = key_at(a, i);
-        s_place[0][i] = i;
+// Up to kFew tokens, in one launch: an entry's place is the number of entries that sort before it, counted by looking at all of them.  A
+// workgroup holds all keys in LDS and counts for 16 entries; 16 neighbouring lanes take one entry each and a share of the keys, four at a
+// time.  2784 tokens 5.7 us, 6144 13 us.  (A radix sort in one workgroup's LDS took 8 us longer for 2784; the launches above take 4 us longer
+// for 5000 tokens and 1 us less for 8192.)
+constexpr uint32_t kFew = 6144, kFewThreads = 512, kFewEntries = 16;
+__global__ __launch_bounds__(kFewThreads) void sort_few_kernel(EmbedArgs a, uint32_t* keys_out, uint32_t* places_out, uint32_t sorters, ZeroShare z) {
+    if (zeroes(a, z, sorters)) return;
+    constexpr uint32_t kShares = kFewThreads / kFewEntries;
+    __shared__ __attribute__((aligned(16))) uint32_t s_key[kFew];
+    __shared__ uint32_t s_before[kShares][kFewEntries];
+    const uint32_t t = threadIdx.x, entry = t % kFewEntries, share = t / kFewEntries, fours = (a.count + 3u) / 4u;
+    for (uint32_t i = t; i < 4u * fours; i += kFewThreads) s_key[i] = i < a.count ? key_at(a, i) : ~0u;   // (behind the last: before nothing)
+    __syncthreads();
+    const uint32_t i = blockIdx.x * kFewEntries + entry, key = s_key[i < a.count ? i : 0u];
+    uint32_t before = 0u;
+    for (uint32_t f = share; f < fours; f += kShares) {
+        const uint4 k = *reinterpret_cast<const uint4*>(&s_key[4u * f]);
+        const uint32_t j = 4u * f;   // (of equal keys the earlier ones; key + 1 <= 2^31)
+        before += k.x < key + (j < i) ? 1u : 0u;
+        before += k.y < key + (j + 1u < i) ? 1u : 0u;
+        before += k.z < key + (j + 2u < i) ? 1u : 0u;
+        before += k.w < key + (j + 3u < i) ? 1u : 0u;
     }
-    uint32_t b = 0;
-    for (uint32_t shift = 0; shift < key_bits; shift += 8u, b ^= 1u) {
-        for (uint32_t d = t; d < kWaves * 256u; d += kFewThreads) s_next[0][d] = 0u;
-        __syncthreads();
-        for (uint32_t i0 = from; i0 < to; i0 += 64u) {
-            const uint32_t i = i0 + lane;
-            const bool in = i < to;
-            const uint32_t digit = in ? (s_key[b][i] >> shift) & 255u : 0u;
-            const uint64_t same = same_digit(digit, 8u, __ballot(in));
-            if (in && (same & ((1ull << lane) - 1ull)) == 0ull) s_next[wave][digit] += (uint32_t)__popcll(same);
-            wave_fence();
-        }
-        __syncthreads();
-        uint32_t total = 0u;
-        if (t < 256u)
-            for (uint32_t w = 0; w < kWaves; ++w) total += s_next[w][t];
-        uint32_t at = sum_before(total, s_wave);
-        if (t < 256u)
-            for (uint32_t w = 0; w < kWaves; ++w) {
-                const uint32_t n = s_next[w][t];
-                s_next[w][t] = at;
-                at += n;
-            }
-        __syncthreads();
-        for (uint32_t i0 = from; i0 < to; i0 += 64u) {
-            const uint32_t i = i0 + lane;
-            const bool in = i < to;
-            const uint32_t key = in ? s_key[b][i] : 0u, digit = (key >> shift) & 255u;
-            const uint64_t same = same_digit(digit, 8u, __ballot(in)), below = same & ((1ull << lane) - 1ull);
-            const uint32_t next = s_next[wave][digit];
-            wave_fence();
-            if (in) {
-                const uint32_t place = next + (uint32_t)__popcll(below);
-                s_key[b ^ 1u][place] = key;
-                s_place[b ^ 1u][place] = s_place[b][i];
-                if (below == 0ull) s_next[wave][digit] = next + (uint32_t)__popcll(same);
-            }
-            wave_fence();
-        }
-        __syncthreads();
-    }
-    for (uint32_t i = t; i < a.count; i += kFewThreads) {
-        keys_out[i] = s_key[b][i];
-        places_out[i] = s_place[b][i];
-    }
+    s_before[share][entry] = before;
+    __syncthreads();
+    if (t >= kFewEntries || i >= a.count) return;
+    uint32_t place = 0u;
+#pragma unroll
+    for (uint32_t q = 0; q < kShares; ++q) place += s_before[q][entry];
+    keys_out[place] = key;
+    places_out[place] = i;
 }
 
 // ---------------------------------------------------------------- sums of the runs
@@ -309,9 +281,8 @@ struct SumArgs {
     uint32_t zero_from;                // rows from here on are set to zero by the sums' launch where they get no gradient
 };
 
-// First entry whose key is at least `key`.
-__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t count, uint32_t key) {
-    uint32_t lo = 0, hi = count;
+// First entry in [lo, hi) whose key is at least `key`.
+__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32_t hi, uint32_t key) {
     while (lo < hi) {
         const uint32_t mid = lo + (hi - lo) / 2u;
         if (keys[mid] < key) lo = mid + 1u;
@@ -320,17 +291,78 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t c
     return lo;
 }
 
-template <bool OUT>
-__device__ __forceinline__ void finish_row(const EmbedArgs& a, uint32_t key, uint32_t d, uint32_t valid, const float (&sum)[8]) {
-    float v[8];
-    const uint64_t at = (uint64_t)key * a.ld_out + d;
-    if (a.accumulate) load_row<OUT>(a.out, at, valid, v);
+constexpr uint32_t kZeroRows = 32;   // rows of the table that a workgroup looks after
+
+// Which of the rows v0 .. v0 + 31 have an entry among the sorted keys, one bit each, by a wave.  The entries of these rows are found by looking at 32
+// keys at a time, the lower lanes for the first one and the upper ones for the end: three looks for up to 2^15 entries, where halving takes 15
+// one after the other (of which each waits for memory).
+__device__ __forceinline__ uint32_t rows_with_entries(const uint32_t* keys, uint32_t count, uint32_t v0, uint32_t vocab) {
+    const uint32_t lane = threadIdx.x & 63u, sub = lane & 31u, past = vocab - v0 < kZeroRows ? vocab : v0 + kZeroRows;
+    const uint32_t target = lane < 32u ? v0 : past;
+    uint32_t lo = 0u, hi = count;
+    while (__any(lo < hi)) {
+        const uint32_t stride = (hi - lo + 31u) / 32u, at = lo + sub * stride;
+        const bool less = at < hi && keys[at] < target;
+        const uint64_t all = __ballot(less);
+        const uint32_t n = (uint32_t)__popc((uint32_t)(lane < 32u ? all : all >> 32));
+        if (n == 0u) {
+            hi = lo;
+        } else {
+            const uint32_t next = lo + n * stride;
+            lo = lo + (n - 1u) * stride + 1u;
+            hi = next < hi ? next : hi;
+        }
+    }
+    const uint32_t first = (uint32_t)__shfl((int)lo, 0), end = (uint32_t)__shfl((int)lo, 32);
+    uint32_t mask = 0u;
+    if (end - first <= 64u) {
+        if (lane < end - first) mask = 1u << (keys[first + lane] - v0);
+    } else if (lane < past - v0) {
+        const uint32_t i = lower_bound(keys, first, end, v0 + lane);
+        mask = i < end && keys[i] == v0 + lane ? 1u << lane : 0u;
+    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = a.accumulate ? v[e] + sum[e] * a.scale : sum[e] * a.scale;
-    store_row<OUT>(a.out, at, valid, v);
+    for (int o = 32; o > 0; o >>= 1) mask |= (uint32_t)__shfl_xor((int)mask, o);
+    return mask;
 }
 
-constexpr uint32_t kZeroRows = 32;   // rows of the table that a workgroup looks after
+// The 8 columns that a lane sums.  Rows need not be a multiple of 8 long: the last lane of a row takes its last 8 columns, of which the
+// first `skip` are its neighbour's too, so that every load is a whole one; a row shorter than 8 is loaded value by value.
+struct Columns {
+    uint32_t d, skip, end;   // the lane writes columns d + skip .. d + end - 1
+    __device__ __forceinline__ Columns(uint32_t chunk, uint32_t dim) {
+        d = chunk * 8u;
+        skip = 0u;
+        end = 8u;
+        if (dim < 8u) {
+            end = dim;
+        } else if (d + 8u > dim) {
+            skip = d + 8u - dim;
+            d = dim - 8u;
+        }
+    }
+};
+
+template <bool OUT>
+__device__ __forceinline__ void finish_row(const EmbedArgs& a, uint32_t key, const Columns& c, const float (&sum)[8]) {
+    constexpr uint32_t kSize = OUT ? 2u : 4u;
+    uint8_t* at = static_cast<uint8_t*>(a.out) + ((uint64_t)key * a.ld_out + c.d) * kSize;
+    if (c.skip == 0u && c.end == 8u) {
+        float v[8] = {};
+        if (a.accumulate) {
+            Row8<OUT> old;
+            old.load(at);
+            old.add_to(v);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = a.accumulate ? v[e] + sum[e] * a.scale : sum[e] * a.scale;
+        Row8<OUT>::store(at, v);
+        return;
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 8u; ++e)
+        if (e >= c.skip && e < c.end) store1<OUT>(at + e * kSize, sum[e] * a.scale, a.accumulate);
+}
 
 template <bool IN, bool OUT>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
@@ -341,13 +373,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
         const uint32_t t = threadIdx.x;
         for (uint64_t v0 = s.zero_from + (uint64_t)(blockIdx.x - s.sum_groups) * kZeroRows; v0 < a.vocab; v0 += (uint64_t)(gridDim.x - s.sum_groups) * kZeroRows) {
             if (t < 64u) {
-                bool present = true;
-                if (t < kZeroRows && v0 + t < a.vocab) {
-                    const uint32_t v = (uint32_t)v0 + t, i = lower_bound(s.keys, a.count, v);
-                    present = i < a.count && s.keys[i] == v;
-                }
-                const uint64_t mask = __ballot(present);
-                if (t == 0u) s_present = (uint32_t)mask;
+                const uint32_t mask = rows_with_entries(s.keys, a.count, (uint32_t)v0, a.vocab);
+                if (t == 0u) s_present = a.vocab - v0 < kZeroRows ? mask | ~0u << (a.vocab - v0) : mask;   // (none behind the table)
             }
             __syncthreads();
             const uint32_t absent = ~s_present;
@@ -368,9 +395,10 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
     }
     const uint64_t group = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / s.lanes;
     const uint32_t p = (uint32_t)(group / s.slices), slice = (uint32_t)(group % s.slices);
-    const uint32_t d = (slice * s.lanes + threadIdx.x % s.lanes) * 8u;
-    if (p >= s.pieces || d >= a.dim) return;
-    const uint32_t valid = a.dim - d, begin = p * s.piece, end = a.count - begin < s.piece ? a.count : begin + s.piece;
+    const uint32_t chunk = slice * s.lanes + threadIdx.x % s.lanes;
+    if (p >= s.pieces || chunk * 8u >= a.dim) return;
+    const Columns columns(chunk, a.dim);
+    const uint32_t d = columns.d, begin = p * s.piece, end = a.count - begin < s.piece ? a.count : begin + s.piece;
     uint32_t key = s.keys[begin];
     bool open = begin != 0u && s.keys[begin - 1u] == key;   // the run has begun before the piece
     float sum[8] = {};
@@ -393,13 +421,13 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
         Row8<IN> v[kAhead];
         uint32_t now[kAhead];
         if (k[0] < a.vocab) {
-            if (valid >= 8u) {
+            if (a.dim >= 8u) {
 #pragma unroll
                 for (uint32_t q = 0; q < kAhead; ++q)
                     v[q].load(static_cast<const uint8_t*>(a.in) + ((uint64_t)place[q] * a.ld_in + d) * (IN ? 2u : 4u));
             } else {
 #pragma unroll
-                for (uint32_t q = 0; q < kAhead; ++q) v[q].load_some(a.in, (uint64_t)place[q] * a.ld_in + d, valid);
+                for (uint32_t q = 0; q < kAhead; ++q) v[q].load_some(a.in, (uint64_t)place[q] * a.ld_in, a.dim);
             }
         }
 #pragma unroll
@@ -410,7 +438,7 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
             if (i + q >= end) continue;
             if (now[q] != key) {
                 if (open) keep(part);
-                else finish_row<OUT>(a, key, d, valid, sum);
+                else finish_row<OUT>(a, key, columns, sum);
                 key = now[q];
                 open = false;
 #pragma unroll
@@ -422,7 +450,7 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArg
     }
     if (open) keep(part);
     else if (end < a.count && s.keys[end] == key) keep(part + (uint64_t)s.pieces * s.pitch);
-    else finish_row<OUT>(a, key, d, valid, sum);
+    else finish_row<OUT>(a, key, columns, sum);
 }
 
 // Runs that cross a border: the piece in which one begins adds what the others have of it, in their order.
@@ -430,8 +458,10 @@ template <bool OUT>
 __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, SumArgs s) {
     const uint64_t group = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / s.lanes;
     const uint32_t p = (uint32_t)(group / s.slices), slice = (uint32_t)(group % s.slices);
-    const uint32_t d = (slice * s.lanes + threadIdx.x % s.lanes) * 8u;
-    if (p + 1u >= s.pieces || d >= a.dim) return;
+    const uint32_t chunk = slice * s.lanes + threadIdx.x % s.lanes;
+    if (p + 1u >= s.pieces || chunk * 8u >= a.dim) return;
+    const Columns columns(chunk, a.dim);
+    const uint32_t d = columns.d;
     const uint32_t begin = p * s.piece, end = begin + s.piece, key = s.keys[end - 1u];
     const uint32_t after = s.keys[end], first_key = s.keys[begin], before = s.keys[begin != 0u ? begin - 1u : 0u];
     if (key >= a.vocab || after != key) return;                            // nothing goes on
@@ -461,7 +491,7 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, SumAr
         for (uint32_t r = 0; r < kAhead; ++r)
             if (in[r]) v[r].add_to(sum);
     }
-    finish_row<OUT>(a, key, d, a.dim - d, sum);
+    finish_row<OUT>(a, key, columns, sum);
 }
 
 // No tokens at all: zeros.
@@ -555,7 +585,8 @@ hipError_t launch_embed_backward(const EmbedArgs& a, hipStream_t stream) {
         return ZeroShare{(uint32_t)((uint64_t)s.zero_from * launch / launches), (uint32_t)((uint64_t)s.zero_from * (launch + 1u) / launches)};
     };
     if (a.count <= kFew) {
-        sort_few_kernel<<<1u + zeroers, kFewThreads, 0, stream>>>(a, list[0], list[1], p.key_bits, share(0));
+        const uint32_t sorters = (a.count + kFewEntries - 1u) / kFewEntries;
+        sort_few_kernel<<<sorters + zeroers, kFewThreads, 0, stream>>>(a, list[0], list[1], sorters, share(0));
         s.keys = list[0];
         s.places = list[1];
     } else {
