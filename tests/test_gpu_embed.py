@@ -65,7 +65,8 @@ def _ws(count, vocab, dim):
 
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("count,vocab,dim", [(1, 1, 1), (1, 300, 70), (3, 5, 1000), (63, 2, 8), (200, 50, 130), (1000, 3000, 33),
-                                             (2049, 700, 64), (5000, 70000, 20), (10000, 300, 256), (30000, 40, 24)])
+                                             (2049, 700, 64), (5000, 70000, 20), (10000, 300, 256), (30000, 40, 24),
+                                             (6144, 500, 1001), (6145, 33, 515), (6143, 70000, 9), (700, 40, 7), (65, 100, 2047)])
 def test_gradient_of_whole_numbers_is_exact(kind, count, vocab, dim):
     rng = np.random.default_rng(dim)
     g = rng.integers(-8, 9, (count, dim)).astype(np.float64)
