@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
         const uint32_t x = l & 31u, xb = (x & 0x13u) | (x & 4u) << 1 | (x & 8u) >> 1;   // (rows of B: bits 2 and 3 exchanged)
         const uint32_t key_a = l >> 4 | (wave & 1u) << 2, key_b = ((l >> 4) & 1u) | (wave & 1u) << 1 | (l >> 5) << 2;
         place_tile(tile, tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
-        m0 = tm * BM, n0 = tn * BN;
+        m0 = tm * BM, n0 = a.first_n + tn * BN;
         rows_m = a.M - m0 < BM ? a.M - m0 : BM, rows_n = a.N - n0 < BN ? a.N - n0 : BN;
 #pragma unroll
         for (uint32_t i = 0; i < MF; ++i) {
@@ -423,6 +423,9 @@ __global__ __launch_bounds__(256) void zero_matrix_kernel(Fp8MatmulArgs a) {
 //    Measured, in us with 256 and 128, bf16 and fp32: 2048 x 4096 x 2048 26 and 19, 46 and 30; 3000 x 4096 x 2048 29 and 29, 53 and 45;
 //    4096 x 4096 x 2048 31 and 37, 57 and 58; 4608 x 4096 x 2048 48 and 43, 90 and 67; 7168 x 4096 x 2048 54 and 61, 104 and 96;
 //    1024 x 50304 x 1024 66 and 73, 119 and 118; 16384 x 8192 x 8192 705 and 905; 8192^3 fp32 690 and 740;
+//    The columns of tiles behind whole rounds of 256, if they are at most 512 tiles of 128 x 128, in those and a launch of their own, where that is
+//    shorter (in tiles of 256, of 128 and of both: 1003 x 50257 x 1024 69, 71 and 64 us; 4608 x 4096 x 8192 149, 137 and 123 us, fp32
+//    292, 223 and 220; 9216 x 4096 x 2048 76, 75 and 72 us; with 576 small ones, 6144 x 4096 x 2048, 51, 51 and 57 us);
 //  - short fp32 products of few tiles of 128 x 128: direct, tiles of 64 x 64 (777 x 520 x 1000, 35 tiles: 8.4 and 9.4 us, to bf16
 //    8.0 and 6.8; 512 x 512 x 1536 10.4 and 11.0 us, to bf16 9.8 and 7.6);
 //  - tiles of 128 x 128 otherwise, the blocks along k divided among workgroups where that is expected to be
@@ -432,6 +435,7 @@ __global__ __launch_bounds__(256) void zero_matrix_kernel(Fp8MatmulArgs a) {
 struct Plan {
     uint32_t tile;      // of the tiled kernel: 256 or 128; of the direct one: 64, or 16 (few rows: all of A, 16 of B)
     uint32_t parts;     // among which the blocks along k are divided
+    uint32_t columns;   // of tiles of 256 x 256: those of whole rounds, what is behind them in tiles of 128 x 128; 0: all
 };
 static Plan plan_for(uint64_t M, uint64_t N, uint64_t K, bool bf16) {
     auto tiles = [&](uint64_t rows, uint64_t cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
@@ -442,7 +446,12 @@ static Plan plan_for(uint64_t M, uint64_t N, uint64_t K, bool bf16) {
         return {16u, (uint32_t)(parts > 1u ? parts : 1u)};
     }
     const uint64_t count = tiles(128, 128);
-    if (4.0 * ((tiles(256, 256) + kUnits - 1u) / kUnits) < (bf16 ? 2.8 : 2.12) * (count > 512u ? count / 512.0 : 1.0)) return {256u, 1u};
+    auto small = [&](uint64_t n) { return (bf16 ? 2.8 : 2.12) * (n > 512u ? n / 512.0 : 1.0); };
+    const uint64_t high = (M + 255u) / 256u, all = tiles(256, 256), whole = all / kUnits * kUnits / high;   // columns of tiles in whole rounds
+    const uint64_t rest = whole * 256u < N ? (M + 127u) / 128u * ((N - whole * 256u + 127u) / 128u) : 0u;
+    const double large = 4.0 * ((all + kUnits - 1u) / kUnits), large_and_small = 4.0 * (all / kUnits) + (rest <= 256u ? bf16 ? 2.2 : 1.5 : bf16 ? 3.1 : 2.4);
+    if (whole != 0u && rest != 0u && rest <= 512u && large_and_small < large && large_and_small < small(count)) return {256u, 1u, (uint32_t)whole};
+    if (large < small(count)) return {256u, 1u};
     if (!bf16 && count < 48u && tiles(64, 64) >= 40u && steps <= 12u) return {64u, 1u};
     Plan best{128u, 1u};
     double least = 0.45 * steps;
@@ -488,17 +497,23 @@ hipError_t launch_fp8_matmul(const Fp8MatmulArgs& args, hipStream_t stream) {
     const uint32_t blocks = (a.K + kStep - 1u) / kStep;
     const uint64_t tiles_m = (a.M + plan.tile - 1u) / plan.tile, tiles_n = (a.N + plan.tile - 1u) / plan.tile;
     if (tiles_m * tiles_n > kMaxGrid) return hipErrorInvalidValue;
-    const uint32_t tm = (uint32_t)tiles_m, tn = (uint32_t)tiles_n;
+    uint32_t tm = (uint32_t)tiles_m, tn = plan.columns ? plan.columns : (uint32_t)tiles_n;
+    a.first_n = 0u;
     a.share = (blocks + plan.parts - 1u) / plan.parts;
     const uint32_t parts = (blocks + a.share - 1u) / a.share;
     // (tiles of 256 x 256 are walked by a workgroup on each compute unit)
-    const uint64_t workgroups = plan.tile == 256u && tiles_m * tiles_n > kUnits ? kUnits : tiles_m * tiles_n;
-    const dim3 grid((uint32_t)workgroups, parts);
+    const dim3 grid(plan.tile == 256u && tm * tn > kUnits ? kUnits : tm * tn, parts);
     auto go = [&](auto FA, auto FB, auto EXACT) {
         constexpr int A = decltype(FA)::value, B = decltype(FB)::value;
         constexpr bool E = decltype(EXACT)::value;
         if (plan.tile == 256u) fp8_matmul_tiled_kernel<A, B, E, 4, 4><<<grid, 256, 0, stream>>>(a, tm, tn);
         else fp8_matmul_tiled_kernel<A, B, E, 2, 2><<<grid, 256, 0, stream>>>(a, tm, tn);
+        if (plan.columns) {
+            a.first_n = plan.columns * 256u;
+            tm = (a.M + 127u) / 128u;
+            tn = (a.N - a.first_n + 127u) / 128u;
+            fp8_matmul_tiled_kernel<A, B, E, 2, 2><<<tm * tn, 256, 0, stream>>>(a, tm, tn);
+        }
         return hipGetLastError();
     };
     using I0 = std::integral_constant<int, 0>;

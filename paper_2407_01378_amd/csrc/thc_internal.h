@@ -255,6 +255,7 @@ struct Fp8MatmulArgs {
     uint64_t ldc;
     float* workspace;     // parts x M x fp8_part_pitch(N), where the blocks along k are divided
     uint32_t share;       // blocks of one part, set by the launch
+    uint32_t first_n;     // column of C at which the launch's tiles begin, set by the launch
 };
 inline __host__ __device__ uint64_t fp8_part_pitch(uint64_t N) { return (N + 7) / 8 * 8; }
 uint64_t fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);

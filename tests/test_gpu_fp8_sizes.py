@@ -29,7 +29,7 @@ def _operand(rows, cols, fmt, seed):
 
 @pytest.mark.parametrize("M,N,K", [
     (5600, 5800, 100), (5600, 5800, 130), (5632, 5888, 700), (9000, 4200, 1000),        # several large tiles to a compute unit
-    (600, 50257, 300), (130, 50257, 256),
+    (600, 50257, 300), (130, 50257, 256), (1003, 50257, 200), (4608, 4096, 300), (4500, 4111, 700), (9216, 4096, 260),   # a rest in small ones
     (16, 24575, 260), (16, 24576, 260), (17, 24575, 1100), (1, 50257, 900), (3, 70001, 128),    # few rows
     (32, 4096, 300), (33, 4096, 300), (17, 4097, 5000), (32, 33, 6000), (29, 2048, 8192),
     (16, 4096, 4096), (17, 300, 8000), (128, 128, 70000), (40, 5000, 9000),              # long sums
@@ -52,7 +52,7 @@ def test_exact(M, N, K, out):
     assert (whole == 7.0).all()                  # nothing beside it
 
 
-@pytest.mark.parametrize("M,N,K", [(5632, 5888, 384), (9000, 4200, 1000)])
+@pytest.mark.parametrize("M,N,K", [(5632, 5888, 384), (9000, 4200, 1000), (4608, 4096, 1000)])
 def test_same_bits_on_every_run(M, N, K):
     g = torch.Generator(device=DEV)
     g.manual_seed(3)
