@@ -201,3 +201,15 @@ def test_tables_beyond_4_gib():
     y = torch.empty(count, dim, device=DEV)
     thc.thc_embed_forward(table, tokens, 2.0, y)
     assert torch.equal(y, torch.where(tokens == 0, 0.0, 2.5)[:, None].expand(count, dim))
+
+
+@pytest.mark.parametrize("count,vocab,dim", [(50, 7, 12), (3000, 400, 33), (9000, 400, 72)])
+def test_rows_of_padding_may_hold_anything(count, vocab, dim):
+    tokens = _tokens(count, vocab, "padded")
+    tokens[::5] = vocab + 3
+    g = torch.randint(-4, 5, (count, dim), generator=_gen(2), device=DEV).float()
+    want, _, _ = O.backward(g.double().cpu().numpy(), tokens.cpu().numpy(), 1.0, vocab)
+    g[(tokens < 0) | (tokens >= vocab)] = float("nan")
+    table = torch.empty(vocab, dim, device=DEV)
+    thc.thc_embed_backward(g, tokens, 1.0, table, _ws(count, vocab, dim))
+    assert torch.equal(table.double(), torch.tensor(want, device=DEV))

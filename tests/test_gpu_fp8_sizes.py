@@ -69,3 +69,27 @@ def test_same_bits_on_every_run(M, N, K):
         thc.thc_fp8_matmul(*ops[0], thc.THC_E4M3, *ops[1], thc.THC_E4M3, K, c, ws)
         first = c if first is None else first
         assert torch.equal(c, first)
+
+
+@pytest.mark.parametrize("M,N", [(2, 5), (20, 36), (40, 36), (300, 200)])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_longest_sums(M, N, out):
+    """2^22 along k, all but 5000 of them zero."""
+    K = 1 << 22
+    g = torch.Generator(device=DEV)
+    g.manual_seed(M)
+    at = torch.randperm(K - 1, generator=g, device=DEV)[:4999]
+    at = torch.cat([at, torch.tensor([K - 1], device=DEV)])
+    table = torch.tensor([0xC0, 0xB8, 0, 0x38, 0x40], dtype=torch.uint8, device=DEV)     # -2 .. 2 in e4m3
+    ops = []
+    for rows in (M, N):
+        v = torch.randint(0, 5, (rows, 5000), generator=g, device=DEV)
+        codes = torch.zeros(rows, K, dtype=torch.uint8, device=DEV)
+        codes[:, at] = table[v]
+        scales = torch.full((thc.thc_fp8_scale_bytes(rows, K),), 127, dtype=torch.uint8, device=DEV)
+        ops.append((codes.reshape(-1), scales, (v - 2).double()))
+    want = (ops[0][2] @ ops[1][2].t()).float()
+    ws = torch.full((thc.thc_fp8_matmul_workspace_bytes(M, N, K),), 0xCD, dtype=torch.uint8, device=DEV)
+    c = torch.full((M, N), float("nan"), dtype=out, device=DEV)
+    thc.thc_fp8_matmul(ops[0][0], ops[0][1], thc.THC_E4M3, ops[1][0], ops[1][1], thc.THC_E4M3, K, c, ws)
+    assert torch.equal(c, want.to(out))
