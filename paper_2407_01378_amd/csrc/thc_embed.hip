@@ -28,9 +28,7 @@ __device__ __forceinline__ void load_row(const void* p, uint64_t at, uint32_t va
     if (valid >= 8u) {
         Row8<BF16> r;
         r.load(static_cast<const uint8_t*>(p) + at * (BF16 ? 2u : 4u));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-        r.add_to(v);
+        r.values(v);   // (not added to zeros: -0 would become 0)
         return;
     }
 #pragma unroll
@@ -352,7 +350,7 @@ __device__ __forceinline__ void finish_row(const EmbedArgs& a, uint32_t key, con
         if (a.accumulate) {
             Row8<OUT> old;
             old.load(at);
-            old.add_to(v);
+            old.values(v);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = a.accumulate ? v[e] + sum[e] * a.scale : sum[e] * a.scale;

@@ -155,11 +155,16 @@ struct Row8 {
             w[BF16 ? 0 : 1] = make_uint4(x[4], x[5], x[6], x[7]);
         }
     }
-    __device__ __forceinline__ void add_to(float (&v)[8]) const {
+    __device__ __forceinline__ void values(float (&v)[8]) const {
         const uint32_t x[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[BF16 ? 0 : 1].x, w[BF16 ? 0 : 1].y, w[BF16 ? 0 : 1].z, w[BF16 ? 0 : 1].w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] += BF16 ? (i & 1 ? bf16_high(x[i >> 1]) : bf16_low(x[i >> 1])) : __uint_as_float(x[i]);
+        for (int i = 0; i < 8; ++i) v[i] = BF16 ? (i & 1 ? bf16_high(x[i >> 1]) : bf16_low(x[i >> 1])) : __uint_as_float(x[i]);
+    }
+    __device__ __forceinline__ void add_to(float (&v)[8]) const {
+        float x[8];
+        values(x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += x[i];
     }
     static __device__ __forceinline__ void store(void* c, const float (&v)[8]) {
         if (BF16) {
