@@ -520,10 +520,11 @@ int topkc_scatter_mean(const uint16_t* values, const uint32_t* indices, uint32_t
  *     other call, each with a workspace of its own; a workspace may be in any state;
  *   - sums are formed in fp32 in an order that depends on the sizes and tokens alone: the same
  *     inputs give the same bits, on every run, replay and stream;
- *   - a NaN or an infinity is not an error: it reaches the results as a NaN, see below.
+ *   - a NaN or an infinity is not an error.  An 8-bit matrix gets NaNs for either, see below, and they reach every
+ *     result that their block enters, and no other; the embedding and its gradient pass both on as they are.
  *
  * An 8-bit matrix of rows x cols has two buffers:
- *   codes   rows * thc_fp8_row_bytes(cols) bytes: every row's codes, zeros up to a multiple of 128;
+ *   codes   rows * thc_fp8_row_bytes(cols) bytes: every row's codes, zeros up to a multiple of 128 (but see the last lines);
  *           THC_E4M3: 1 sign, 4 exponent (bias 7), 3 fraction bits, largest value 448, no infinity;
  *           THC_E5M2: 1, 5 (bias 15) and 2 bits, largest value 57344
  *   scales  thc_fp8_scale_bytes(rows, cols) bytes: block j = c / 128 of row r has the scale
@@ -533,7 +534,10 @@ int topkc_scatter_mean(const uint16_t* values, const uint32_t* indices, uint32_t
  * rounds: e is the smallest byte for which the block's largest magnitude amax does not exceed the
  * format's largest value times 2^(e - 127) (0 for an amax of up to 1.75 * 2^-119 with e4m3,
  * 1.75 * 2^-112 with e5m2), and a code is the value times 2^(127 - e), rounded to nearest, ties to
- * even.  A block with a NaN or an infinity gets e = 255 and the NaN code 0x7F throughout.  Both buffers 16-byte aligned. */
+ * even.  Both buffers 16-byte aligned.
+ * A block with a NaN or an infinity gets e = 255 and the NaN code 0x7F throughout, behind the row's last column too.
+ * Where a caller writes the buffers itself: a block with e = 255 is NaN whatever its codes are, and a code that is a NaN or (e5m2) an
+ * infinity counts as that. */
 enum { THC_E4M3 = 0, THC_E5M2 = 1 };
 enum { THC_I32 = 0, THC_I64 = 1 };   /* type of token indices, signed */
 

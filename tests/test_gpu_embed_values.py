@@ -1,4 +1,4 @@
-"""Embedding lookup and gradient: zeros keep their sign."""
+"""Embedding lookup and gradient: zeros keep their sign, infinities stay infinities."""
 import pytest
 import torch
 
@@ -43,3 +43,31 @@ def test_zeros_that_are_added_to(dim, out):
                 want = torch.full((9, dim), old, dtype=out, device=DEV)
                 want[:5] = old + scale * 0.0
                 assert torch.equal(grad.view(BITS[out]), want.view(BITS[out]))
+
+
+@pytest.mark.parametrize("dim", [5, 16, 1001])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_values_that_are_not_finite(dim, out):
+    inf, nan = float("inf"), float("nan")
+    table = torch.ones(12, dim, device=DEV)
+    table[1, 0], table[2, dim - 1], table[3, 1] = inf, -inf, nan
+    tokens = torch.tensor([3, 2, 1, 0, -1, 12], device=DEV)
+    y = torch.empty(6, dim, dtype=out, device=DEV)
+    thc.thc_embed_forward(table, tokens, -2.0, y)
+    want = table[tokens.clamp(0, 11)] * -2.0
+    want[4:] = 0.0
+    assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.float().nan_to_num(nan=0.5), want.nan_to_num(nan=0.5))
+    for count in (40, 7000):                                # both ways to sort
+        g = torch.ones(count, dim, device=DEV)
+        tokens = torch.arange(count, device=DEV) % 10
+        g[13, 0], g[24, dim - 1], g[37, 1], g[17, 1] = inf, -inf, inf, -inf
+        g[15, 0] = nan
+        grad = torch.empty(12, dim, dtype=out, device=DEV)
+        ws = torch.empty(thc.thc_embed_backward_workspace_bytes(count, 12, dim), dtype=torch.uint8, device=DEV)
+        thc.thc_embed_backward(g, tokens, -1.0, grad, ws)
+        want = torch.zeros(12, dim, device=DEV)
+        want[:10] = -float(count // 10)
+        want[3, 0], want[4, dim - 1], want[7, 1], want[5, 0] = -inf, inf, nan, nan
+        want = want.to(out)
+        assert torch.equal(grad.isnan(), want.isnan())
+        assert torch.equal(grad.float().nan_to_num(nan=0.5), want.float().nan_to_num(nan=0.5))
