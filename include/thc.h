@@ -576,7 +576,7 @@ int thc_fp8_dequantize(const uint8_t* q, const uint8_t* scales, int format, uint
  *   workspace     thc_fp8_matmul_workspace_bytes(M, N, K) bytes, 16-byte aligned; may be NULL if that is 0
  * A linear layer with weights W (N x K) has  y = x W^T,  dx = dy (W^T)^T  (contracted over N) and
  * dW = (dy^T) (x^T)^T  (contracted over the tokens): thc_fp8_quantize writes every operand in the
- * form that is wanted.  M, N <= 2^26, K <= 2^22 (THC_ERR_SIZE).  K == 0: an empty sum. */
+ * form that is wanted.  M, N <= 2^26, M * N <= 2^39, K <= 2^22 (THC_ERR_SIZE).  K == 0: an empty sum. */
 uint64_t thc_fp8_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
 int thc_fp8_matmul(const uint8_t* a, const uint8_t* a_scales, int a_format, const uint8_t* b, const uint8_t* b_scales,
                    int b_format, uint64_t M, uint64_t N, uint64_t K, int accumulate, thc_dtype out_dt, void* c,

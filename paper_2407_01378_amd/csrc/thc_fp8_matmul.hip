@@ -24,7 +24,6 @@ namespace {
 
 constexpr uint32_t kStep = 128;
 constexpr uint32_t kUnits = 256;   // compute units (a multiple of the dies, so that a workgroup's tiles are its die's)
-constexpr uint64_t kMaxGrid = 1ull << 23;   // workgroups of 256 threads: 2^31 threads
 
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -495,9 +494,7 @@ hipError_t launch_fp8_matmul(const Fp8MatmulArgs& args, hipStream_t stream) {
         return launch_fp8_direct(direct, stream);
     }
     const uint32_t blocks = (a.K + kStep - 1u) / kStep;
-    const uint64_t tiles_m = (a.M + plan.tile - 1u) / plan.tile, tiles_n = (a.N + plan.tile - 1u) / plan.tile;
-    if (tiles_m * tiles_n > kMaxGrid) return hipErrorInvalidValue;
-    uint32_t tm = (uint32_t)tiles_m, tn = plan.columns ? plan.columns : (uint32_t)tiles_n;
+    uint32_t tm = (a.M + plan.tile - 1u) / plan.tile, tn = plan.columns ? plan.columns : (a.N + plan.tile - 1u) / plan.tile;
     a.first_n = 0u;
     a.share = (blocks + plan.parts - 1u) / plan.parts;
     const uint32_t parts = (blocks + a.share - 1u) / a.share;
