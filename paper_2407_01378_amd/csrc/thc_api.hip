@@ -1170,7 +1170,7 @@ int thc_fp8_dequantize(const uint8_t* q, const uint8_t* scales, int format, uint
                                              static_cast<hipStream_t>(stream)));
 }
 
-static constexpr uint64_t kMaxProductRows = 1ull << 26;    // of A and of B: 2^22 workgroups for a single row of the other
+static constexpr uint64_t kMaxProductRows = 1ull << 26;    // of A and of B: 2^19 tiles of 128 rows for one column of them
 static constexpr uint64_t kMaxProductValues = 1ull << 39;  // of C: at most 2^23 tiles to a launch that has a workgroup for each
 static bool fp8_product_in_range(uint64_t M, uint64_t N, uint64_t K) {
     return M <= kMaxProductRows && N <= kMaxProductRows && M * N <= kMaxProductValues && K <= kMaxContracted;

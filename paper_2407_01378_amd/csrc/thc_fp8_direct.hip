@@ -225,7 +225,8 @@ hipError_t launch_fp8_direct(const Fp8DirectArgs& args, hipStream_t stream) {
     const bool few = fp8_rows_are_few(a.M, a.N, a.K);
     const uint32_t cols = few ? 16u : 64u, rows = few && a.M > 16u ? 32u : cols, wanted = few ? fp8_few_rows_parts(a.M, a.N, a.K) : 1u, steps = (a.K + 127u) / 128u;
     const uint32_t tiles_m = (a.M + rows - 1u) / rows, tiles_n = (a.N + cols - 1u) / cols;
-    if (steps == 0u || (uint64_t)tiles_m * tiles_n > (1u << 22) || (a.source != 0u && !(few && rows == 16u))) return hipErrorInvalidValue;
+    // (few rows: at most 1536 workgroups along B, tiles of 64: fewer than 192)
+    if (steps == 0u || (a.source != 0u && !(few && rows == 16u))) return hipErrorInvalidValue;   // (no caller asks for it)
     a.share = (steps + wanted - 1u) / wanted;
     const uint32_t parts = (steps + a.share - 1u) / a.share;
     const dim3 grid(tiles_m * tiles_n, parts);
