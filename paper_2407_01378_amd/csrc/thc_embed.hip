@@ -464,8 +464,10 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedArgs a, SumAr
     const uint32_t after = s.keys[end], first_key = s.keys[begin], before = s.keys[begin != 0u ? begin - 1u : 0u];
     if (key >= a.vocab || after != key) return;                            // nothing goes on
     if (first_key == key && begin != 0u && before == key) return;          // it has begun before
-    float sum[8];
-    load_row<false>(s.parts, ((uint64_t)s.pieces + p) * s.pitch + d, 8u, sum);
+    float sum[8] = {};
+    Row8<false> mine;   // (added to zeros, as no part is -0: loaded in place the sum is waited for in every branch below, 13 us instead of 7)
+    mine.load(s.parts + ((uint64_t)s.pieces + p) * s.pitch + d);
+    mine.add_to(sum);
     // pieces that begin with the run, 16 at a time; their parts are loaded where there are such pieces (most runs end in the next one)
     constexpr uint32_t kAhead = 16;
     uint32_t first[kAhead];
