@@ -570,7 +570,8 @@ int thc_fp8_dequantize(const uint8_t* q, const uint8_t* scales, int format, uint
  *   out_dt THC_F32: products are exact; a value beyond the normal range of fp32 counts as zero or infinite.
  *   out_dt THC_BF16: of the products of 8 neighbouring k what lies more than 2^13 below the largest of them may be
  *   cut off (the 8-bit matrix instruction; on normally distributed values 1.5e-5 in the 2-norm, of
- *   the 1.7e-3 that the rounding to bf16 costs).
+ *   the 1.7e-3 that the rounding to bf16 costs; at most 7 * 2^-13 of the sum of the products' magnitudes, which a
+ *   result that nearly cancels can see.  Where that matters: THC_F32).
  *   a, a_scales   8-bit matrix of M x K;   b, b_scales   8-bit matrix of N x K
  *   c             M x N of out_dt, ldc
  *   workspace     thc_fp8_matmul_workspace_bytes(M, N, K) bytes, 16-byte aligned; may be NULL if that is 0

@@ -359,7 +359,10 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_tiled_kernel(Fp8MatmulArgs 
             begin();
         }
         // Whole tiles leave in a known number of stores, which are still on their way when the next tile begins: only its first two steps,
-        // fetched before them, are waited for.
+        // fetched before them, are waited for.  (They are waited for sooner than here: the compiler does not know a strip from the units
+        // that are fetched to, and waits for all fetches before the first write to a strip.)
+        // Tiles that are added to what is there take the ragged way out, piece by piece: 8192 x 8192 x 2048 373 us for 219 to fp32, 265 for
+        // 115 to bf16; 2048 x 8192 x 8192 218 for 191 and 117 for 94.
         using yes = std::true_type;
         using no = std::false_type;
         const bool whole = m + BM <= a.M && n + BN <= a.N && !a.accumulate;

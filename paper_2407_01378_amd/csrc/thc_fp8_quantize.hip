@@ -5,7 +5,7 @@
 // LDS).  Both forms, along the rows and along the columns, come from one read of x; the codes of the
 // transposed form pass through LDS so that every store is a whole piece of a row.
 // What bounds it: memory, 2 or 4 bytes read and 1 written per value and form.  Measured: 8192 x 8192 bf16, both forms, 61 us and
-// 8192 x 2048 fp32 by tiles, both forms, 23 us, 4.4 TB/s each (a 4 GiB copy reaches 4.7); back from codes 14.5 us (8192 x 2048 to fp32).  A
+// 8192 x 2048 fp32 by tiles, both forms, 23 us, 4.4 TB/s each (a 4 GiB copy reaches 4.7); 8192 x 8192 bf16 along the rows only 42 us, 4.9 TB/s; back from codes 14.5 us (8192 x 2048 to fp32).  A
 // small matrix, of fewer tiles than compute units, takes 6 us whatever its size: one tile's way through memory and LDS.
 #include "thc_device.h"
 #include "thc_fp8.h"
